@@ -436,6 +436,93 @@ int neus2_march_rays(int log2_res, const uint32_t* bitfield, const float* origin
                      const float* jitter, int64_t rays, float dt, int32_t max_steps, int64_t capacity,
                      int32_t* ray_offsets, float* pos, int32_t* sample_ray, float* t, void* stream);
 
+/* ---- Layers whose rows choose their matrices -----------------------------------------------------
+ * The networks above have one set of matrices for a whole batch.  Programs with many frames, views,
+ * objects or blocks of space in one batch want matrices of their own for each group of consecutive
+ * rows (samples), or one shared matrix and a low-rank residual for each group: a bias-free layer
+ * y = g(W x) of Definition 1 of any width, with first-order gradients (all that the paper's colour
+ * network needs; the SDF's second-order term has no form here).  Layers are chained by the caller.
+ *
+ * Rows: group g owns rows offsets[g] .. offsets[g+1]-1 of the n rows (offsets [device, groups+1
+ *   int32], non-decreasing, 0..n); any count, also 0.  Rows before the first and behind the last
+ *   group are neither read nor written.  offsets may be NULL with one group: all n rows.  Offsets are
+ *   cut to 0..n on the device: wrong ones give wrong results, never an access outside the arrays.
+ * Types: x, y, dx, dy, W, A, B have the layer's dtype; sums are fp32 (fp32 factors: three bf16 terms,
+ *   as accurate as an fp32 product); gradients of matrices, u and scales are fp32.  An infinite fp32
+ *   factor gives NaN in the results it enters.
+ * Row strides: x_stride, y_stride count values from one row to the next (0: in_dim, out_dim); dx has
+ *   x's, dy has y's.  Any stride works, multiples of 16 bytes are the fast ones.
+ * accumulate: matrix gradients are ADDED into (1) or overwritten (0: groups without rows get zeros).
+ * n = 0: the arrays of rows may be NULL; matrix gradients are zeroed or left as they are.
+ * Results do not depend on the order in which workgroups run. */
+typedef struct neus2_layer {
+    int32_t dtype;             /* 0 = fp32, 1 = fp16, 2 = bf16 */
+    int32_t groups;            /* groups of consecutive rows, 1..2^20 */
+    int32_t in_dim, out_dim;   /* 1..65536 */
+    int32_t rank;              /* adapters: 1..64; 0 for a grouped layer */
+    int32_t adapters;          /* adapters: matrices in the bank, 1..2^20; 0 for a grouped layer */
+    int32_t relu;              /* 1: y = max(W x, 0) */
+    int32_t accumulate;
+    int64_t x_stride, y_stride;
+} neus2_layer;
+
+/* y_i = g(W_g x_i) for the rows i of group g.  x [device, n rows], W [device, groups*out_dim*in_dim],
+ * y [device, n rows]. */
+int neus2_grouped_fwd(const neus2_layer* layer /*[host]*/, const void* x, const void* W, const int32_t* offsets,
+                      int64_t n, void* y, void* stream);
+
+/* Its gradients: dx_i = W_g^T dy_i (zero where masks, if given, has no bit), dW_g (+)= sum dy_i x_i^T.
+ *   dy: the gradient in front of the layer's own ReLU, that is with the masks of y applied; the call of
+ *     the layer above does that when it is handed those as its `masks` ("of its input").
+ *   x [device, n rows], or x NULL and xq, xe [device]: the layer's input as neus2_pack8 stored it.
+ *   masks [device, n*ceil(in_dim/32) uint32] or NULL: as neus2_pack8 writes them for x, the ReLU masks of
+ *     the layer below.
+ *   dx or dW may be NULL: not wanted (then W, x are not needed).
+ *   dW [device, groups*out_dim*in_dim fp32]; workspace [device, at least neus2_grouped_workspace_bytes
+ *   (layer, n)], may be NULL if that is 0; contents are undefined afterwards.  The size query returns -1
+ *   on a bad descriptor or n. */
+int64_t neus2_grouped_workspace_bytes(const neus2_layer* layer /*[host]*/, int64_t n);
+int neus2_grouped_bwd(const neus2_layer* layer /*[host]*/, const void* x, const int8_t* xq, const uint8_t* xe,
+                      const uint32_t* masks, const void* W, const int32_t* offsets, const void* dy, int64_t n,
+                      void* dx, float* dW, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* A shared matrix and adapters: u_i = scales[s] A_s x_i, y_i = g(W x_i + B_s u_i), where s = slots[g] is
+ * the adapter of row i's group g.
+ *   W [device, out_dim*in_dim]; the bank: A [device, adapters*rank*in_dim], B [device,
+ *   adapters*out_dim*rank], scales [device, adapters fp32]; smaller ranks are filled up with zeros.
+ *   slots [device, groups int32] or NULL (group g has adapter g): any slot may be named by any number of
+ *   groups; one outside 0..adapters-1 (-1) means none: y_i = g(W x_i), u_i = 0.
+ *   offsets is required.  u [device, n*rank fp32]: written, for the backward call or as scratch. */
+int neus2_adapter_fwd(const neus2_layer* layer /*[host]*/, const void* x, const void* W, const void* A, const void* B,
+                      const float* scales, const int32_t* slots, const int32_t* offsets, int64_t n, float* u, void* y,
+                      void* stream);
+
+/* Its gradients, W staying as it is (neus2_grouped_bwd with one group gives dW): v_i = scales[s] B_s^T dy_i,
+ * dx_i = W^T dy_i + A_s^T v_i (masks as above), dA_s (+)= sum v_i x_i^T, dB_s (+)= sum dy_i u_i^T over all
+ * rows of all groups with slot s.  x / xq, xe, masks, dy as in neus2_grouped_bwd; u as the forward call wrote it;
+ *   dA, dB shaped like A, B, fp32, both or neither; dx NULL: not wanted.  workspace [device, at least
+ *   neus2_adapter_workspace_bytes(layer, n)]: required. */
+int64_t neus2_adapter_workspace_bytes(const neus2_layer* layer /*[host]*/, int64_t n);
+int neus2_adapter_bwd(const neus2_layer* layer /*[host]*/, const void* x, const int8_t* xq, const uint8_t* xe,
+                      const uint32_t* masks, const void* W, const void* A, const void* B, const float* scales,
+                      const int32_t* slots, const int32_t* offsets, const float* u, const void* dy, int64_t n, void* dx,
+                      float* dA, float* dB, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* What a layer keeps of its input for the backward pass, in 8 bits: for every row and block of 32 features the
+ * smallest power of two 2^t (t >= -126) of which the largest magnitude is at most 127 steps after rounding, and
+ * every feature as a whole number of steps (ties to even), off by at most half of one.
+ *   x [device, n rows of dim values, x_stride as above] fp32, fp16 or bf16 (dtype);
+ *   q [device, n*32*ceil(dim/32) int8]: the steps, zeros behind the last feature;
+ *   e [device, n*ceil(dim/32) uint8]: t + 127; 255: the block held an infinity or a NaN and comes back as NaN;
+ *   masks [device, n*ceil(dim/32) uint32] or NULL: bit c%32 of word c/32 = (x_c > 0), the ReLU masks of the
+ *   layer that made x.  With masks q and e may both be NULL: the masks alone.
+ * (Where the 64th step is beyond the type's largest number, magnitudes are cut to 63 steps.)
+ * neus2_unpack8: x = q 2^t, exact in all three types. */
+int neus2_pack8(int32_t dtype, const void* x, int64_t x_stride, int64_t n, int32_t dim, int8_t* q, uint8_t* e,
+                uint32_t* masks, void* stream);
+int neus2_unpack8(int32_t dtype, const int8_t* q, const uint8_t* e, int64_t n, int32_t dim, void* x,
+                  int64_t x_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

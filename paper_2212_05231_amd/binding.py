@@ -44,6 +44,11 @@ class Neus2StepBuffers(C.Structure):
         ("n_rays", C.c_int64), ("sdf_masks", _P), ("color_masks", _P)]
 
 
+class Neus2Layer(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("dtype", "groups", "in_dim", "out_dim", "rank", "adapters", "relu", "accumulate")] + [
+        ("x_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
 class Neus2Error(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"libneus2: {ERROR_NAMES.get(code, code)}: {message}")
@@ -93,6 +98,14 @@ _SIGNATURES = {
     "neus2_occupancy_update_ordered": (C.c_int, [C.c_int, _P, _P, _P, C.c_int64, _P, _P, C.c_float, C.c_float, C.c_float, _P, _P]),
     "neus2_occupancy_update": (C.c_int, [C.c_int, _P, _P, _P, C.c_int64, C.c_int64, _P, C.c_float, C.c_float, C.c_float, _P, _P]),
     "neus2_march_rays": (C.c_int, [C.c_int, _P, _P, _P, _P, C.c_int64, C.c_float, C.c_int32, C.c_int64, _P, _P, _P, _P, _P]),
+    "neus2_grouped_fwd": (C.c_int, [C.POINTER(Neus2Layer), _P, _P, _P, C.c_int64, _P, _P]),
+    "neus2_grouped_workspace_bytes": (C.c_int64, [C.POINTER(Neus2Layer), C.c_int64]),
+    "neus2_grouped_bwd": (C.c_int, [C.POINTER(Neus2Layer), _P, _P, _P, _P, _P, _P, _P, C.c_int64, _P, _P, _P, C.c_int64, _P]),
+    "neus2_adapter_fwd": (C.c_int, [C.POINTER(Neus2Layer), _P, _P, _P, _P, _P, _P, _P, C.c_int64, _P, _P, _P]),
+    "neus2_adapter_workspace_bytes": (C.c_int64, [C.POINTER(Neus2Layer), C.c_int64]),
+    "neus2_adapter_bwd": (C.c_int, [C.POINTER(Neus2Layer)] + [_P] * 12 + [C.c_int64, _P, _P, _P, _P, C.c_int64, _P]),
+    "neus2_pack8": (C.c_int, [C.c_int32, _P, C.c_int64, C.c_int64, C.c_int32, _P, _P, _P, _P]),
+    "neus2_unpack8": (C.c_int, [C.c_int32, _P, _P, C.c_int64, C.c_int32, _P, C.c_int64, _P]),
     "neus2_train_step": (C.c_int, [C.POINTER(Neus2Config), C.POINTER(Neus2StepBuffers), C.c_int64, _P]),
 }
 
@@ -334,6 +347,191 @@ def march_rays(log2_res, bitfield, origins, dirs, jitter, dt, max_steps, capacit
     _check(lib().neus2_march_rays(log2_res, _ptr(bitfield), _ptr(origins), _ptr(dirs), _ptr(jitter), origins.shape[0],
                                   dt, max_steps, capacity, _ptr(ray_offsets), _ptr(pos), _ptr(sample_ray), _ptr(t),
                                   _stream()))
+
+
+# ---- layers whose rows choose their matrices ---------------------------------------------------
+LAYER_TYPES = ("f32", "f16", "bf16")
+
+
+def make_layer(dtype, groups, in_dim, out_dim, rank=0, adapters=0, relu=False, accumulate=False, x_stride=0, y_stride=0) -> Neus2Layer:
+    """Descriptor of a grouped layer (rank 0) or of one with adapters; `dtype` is "f32", "f16" or "bf16"."""
+    return Neus2Layer(LAYER_TYPES.index(dtype), groups, in_dim, out_dim, rank, adapters, int(relu), int(accumulate), x_stride, y_stride)
+
+
+def _dtype_of(t) -> int:
+    import torch
+    try:
+        return (torch.float32, torch.float16, torch.bfloat16).index(t.dtype)
+    except ValueError:
+        raise ValueError(f"{t.dtype}: rows are fp32, fp16 or bf16") from None
+
+
+def _check_tensor(t, name, shape, dtype, device) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, expected {tuple(shape)} of {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _check_rows(t, name, n, dim, stride, dtype, device) -> None:
+    """[n, dim] with rows `stride` values apart (0: dim)."""
+    if tuple(t.shape) != (n, dim) or t.dtype != dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, expected {(n, dim)} of {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if n > 0 and dim > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) != (stride or dim):
+        raise ValueError(f"{name}: strides {t.stride()}, expected {(stride or dim, 1)}")
+
+
+def _current_device(t, name):
+    import torch
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.device
+
+
+def _layer_dtype(layer):
+    import torch
+    return (torch.float32, torch.float16, torch.bfloat16)[layer.dtype]
+
+
+def _check_offsets(layer, offsets, device) -> None:
+    import torch
+    if offsets is not None:
+        _check_tensor(offsets, "offsets", (layer.groups + 1,), torch.int32, device)
+
+
+def _layer_input(layer, x, n, device):
+    """x or its packed form (q, e) -> the three pointers x, xq, xe."""
+    import torch
+    if isinstance(x, (tuple, list)):
+        q, e = x
+        blocks = (layer.in_dim + 31) // 32
+        _check_tensor(q, "xq", (n, 32 * blocks), torch.int8, device)
+        _check_tensor(e, "xe", (n, blocks), torch.uint8, device)
+        return None, q.data_ptr(), e.data_ptr()
+    if x is None:
+        return None, None, None
+    _check_rows(x, "x", n, layer.in_dim, layer.x_stride, _layer_dtype(layer), device)
+    return x.data_ptr(), None, None
+
+
+def _check_masks(layer, masks, n, device) -> None:
+    import torch
+    if masks is not None:
+        _check_tensor(masks, "masks", (n, (layer.in_dim + 31) // 32), torch.int32, device)
+
+
+def _data(t):
+    return None if t is None else t.data_ptr()
+
+
+def grouped_fwd(layer, x, W, offsets, y) -> None:
+    device, dtype, n = _current_device(x, "x"), _layer_dtype(layer), x.shape[0]
+    _check_rows(x, "x", n, layer.in_dim, layer.x_stride, dtype, device)
+    _check_tensor(W, "W", (layer.groups, layer.out_dim, layer.in_dim), dtype, device)
+    _check_offsets(layer, offsets, device)
+    _check_rows(y, "y", n, layer.out_dim, layer.y_stride, dtype, device)
+    _check(lib().neus2_grouped_fwd(C.byref(layer), _data(x), _data(W), _data(offsets), n, _data(y), _stream()))
+
+
+def grouped_workspace_bytes(layer, n: int) -> int:
+    return lib().neus2_grouped_workspace_bytes(C.byref(layer), n)
+
+
+def grouped_bwd(layer, x, W, offsets, dy, dx, dW, workspace=None, masks=None) -> None:
+    """`x` is the layer's input, its packed form (q, e), or None if dW is; `dx`, `dW` may be None."""
+    import torch
+    device, dtype, n = _current_device(dy, "dy"), _layer_dtype(layer), dy.shape[0]
+    _check_rows(dy, "dy", n, layer.out_dim, layer.y_stride, dtype, device)
+    xp, xq, xe = _layer_input(layer, x, n, device)
+    if W is not None:
+        _check_tensor(W, "W", (layer.groups, layer.out_dim, layer.in_dim), dtype, device)
+    _check_offsets(layer, offsets, device)
+    _check_masks(layer, masks, n, device)
+    if dx is not None:
+        _check_rows(dx, "dx", n, layer.in_dim, layer.x_stride, dtype, device)
+    if dW is not None:
+        _check_tensor(dW, "dW", (layer.groups, layer.out_dim, layer.in_dim), torch.float32, device)
+    _check(lib().neus2_grouped_bwd(C.byref(layer), xp, xq, xe, _data(masks), _data(W), _data(offsets), _data(dy), n, _data(dx),
+                                   _data(dW), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def _check_bank(layer, A, B, scales, slots, offsets, device) -> None:
+    import torch
+    dtype = _layer_dtype(layer)
+    _check_tensor(A, "A", (layer.adapters, layer.rank, layer.in_dim), dtype, device)
+    _check_tensor(B, "B", (layer.adapters, layer.out_dim, layer.rank), dtype, device)
+    _check_tensor(scales, "scales", (layer.adapters,), torch.float32, device)
+    if slots is not None:
+        _check_tensor(slots, "slots", (layer.groups,), torch.int32, device)
+    _check_tensor(offsets, "offsets", (layer.groups + 1,), torch.int32, device)
+
+
+def adapter_fwd(layer, x, W, A, B, scales, slots, offsets, u, y) -> None:
+    import torch
+    device, dtype, n = _current_device(x, "x"), _layer_dtype(layer), x.shape[0]
+    _check_rows(x, "x", n, layer.in_dim, layer.x_stride, dtype, device)
+    _check_tensor(W, "W", (layer.out_dim, layer.in_dim), dtype, device)
+    _check_bank(layer, A, B, scales, slots, offsets, device)
+    _check_tensor(u, "u", (n, layer.rank), torch.float32, device)
+    _check_rows(y, "y", n, layer.out_dim, layer.y_stride, dtype, device)
+    _check(lib().neus2_adapter_fwd(C.byref(layer), _data(x), _data(W), _data(A), _data(B), _data(scales), _data(slots), _data(offsets),
+                                   n, _data(u), _data(y), _stream()))
+
+
+def adapter_workspace_bytes(layer, n: int) -> int:
+    return lib().neus2_adapter_workspace_bytes(C.byref(layer), n)
+
+
+def adapter_bwd(layer, x, W, A, B, scales, slots, offsets, u, dy, dx, dA, dB, workspace, masks=None) -> None:
+    """`x` as in grouped_bwd; `dx`, or `dA` and `dB`, may be None."""
+    import torch
+    device, dtype, n = _current_device(dy, "dy"), _layer_dtype(layer), dy.shape[0]
+    _check_rows(dy, "dy", n, layer.out_dim, layer.y_stride, dtype, device)
+    xp, xq, xe = _layer_input(layer, x, n, device)
+    if W is not None:
+        _check_tensor(W, "W", (layer.out_dim, layer.in_dim), dtype, device)
+    _check_bank(layer, A, B, scales, slots, offsets, device)
+    _check_masks(layer, masks, n, device)
+    if u is not None:
+        _check_tensor(u, "u", (n, layer.rank), torch.float32, device)
+    if dx is not None:
+        _check_rows(dx, "dx", n, layer.in_dim, layer.x_stride, dtype, device)
+    for t, name, like in ((dA, "dA", A), (dB, "dB", B)):
+        if t is not None:
+            _check_tensor(t, name, like.shape, torch.float32, device)
+    _check(lib().neus2_adapter_bwd(C.byref(layer), xp, xq, xe, _data(masks), _data(W), _data(A), _data(B), _data(scales), _data(slots),
+                                   _data(offsets), _data(u), _data(dy), n, _data(dx), _data(dA), _data(dB), _ptr(workspace),
+                                   _bytes(workspace), _stream()))
+
+
+def _check_packed_form(q, e, masks, n, dim, device) -> None:
+    import torch
+    blocks = (dim + 31) // 32
+    if q is not None or e is not None or masks is None:
+        _check_tensor(q, "q", (n, 32 * blocks), torch.int8, device)
+        _check_tensor(e, "e", (n, blocks), torch.uint8, device)
+    if masks is not None:
+        _check_tensor(masks, "masks", (n, blocks), torch.int32, device)
+
+
+def pack8(x, q, e, masks=None) -> None:
+    """x [n, dim] (rows any distance apart) -> q [n, 32 * blocks] int8, e [n, blocks] uint8, masks [n, blocks] int32;
+    q and e None: the masks alone."""
+    device, (n, dim) = _current_device(x, "x"), x.shape
+    _check_rows(x, "x", n, dim, x.stride(0) if n > 1 else 0, x.dtype, device)
+    _check_packed_form(q, e, masks, n, dim, device)
+    _check(lib().neus2_pack8(_dtype_of(x), _data(x), x.stride(0) if n > 1 else 0, n, dim, _data(q), _data(e), _data(masks), _stream()))
+
+
+def unpack8(q, e, x) -> None:
+    device, (n, dim) = _current_device(x, "x"), x.shape
+    _check_rows(x, "x", n, dim, x.stride(0) if n > 1 else 0, x.dtype, device)
+    _check_packed_form(q, e, None, n, dim, device)
+    _check(lib().neus2_unpack8(_dtype_of(x), _data(q), _data(e), n, dim, _data(x), x.stride(0) if n > 1 else 0, _stream()))
 
 
 class Step:

@@ -13,6 +13,7 @@ namespace neus2 {
 int fail(int code, const char* fmt, ...);           // records the message, returns code
 int check_config(const neus2_config* cfg);
 int check_ptr(const void* p, const char* name, bool required = true);
+int check_count(int64_t n, const char* name);        // 0..2^28
 int check_launch(const char* what);                  // hipGetLastError -> NEUS2_ERR_HIP
 
 #define NEUS2_TRY(expr)                 \

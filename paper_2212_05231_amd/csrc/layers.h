@@ -1,0 +1,349 @@
+// Building blocks of the layers whose rows choose their matrices (layers.hip, layers_grad.hip): where the rows of a group
+// lie, and tiles of a product's two factors in LDS, ready for the 32x32x16 matrix instructions.
+//
+// Types.  bf16 and fp16 factors go to the matrix cores as they are, one instruction per k-step, accumulated in fp32.  fp32
+// factors are sums of bf16 terms as in mfma_tile.h: three terms and six products, as accurate as an fp32 product.  Where a
+// factor kept in fp32 (an adapter's u or v) meets one of 16 bits, the fp32 one takes two terms (2^-17 relative, below the
+// 2^-9 or 2^-12 with which the other factor came) and an fp16 one is two bf16 terms (8 + 8 >= 11 bits: exact), so that
+// small gradients do not fall out of fp16's range.  An infinite fp32 factor makes its products NaN (inf - inf in the split).
+#pragma once
+
+#include "common.h"
+#include "mfma_tile.h"
+
+namespace neus2 {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+enum : int { kTypeF32 = 0, kTypeF16 = 1, kTypeBF16 = 2 };
+
+template <int DT> struct TypeOf;
+template <> struct TypeOf<kTypeF32> { typedef float Element; };
+template <> struct TypeOf<kTypeF16> { typedef _Float16 Element; };
+template <> struct TypeOf<kTypeBF16> { typedef __bf16 Element; };
+
+// ---- groups of consecutive rows ----------------------------------------------------------------------------------------
+// Group g owns rows offsets[g] .. offsets[g+1] - 1.  Offsets come from device memory, so whatever they hold is cut to 0..n
+// here: a wrong one may leave rows out, it never leads outside the arrays.
+struct RowGroups {
+    const int32_t* offsets;     // NULL: one group, all n rows
+    int32_t groups;
+    int32_t n;
+    int32_t whole;              // 1: the rows of all groups taken as one group (offsets[0] .. offsets[groups])
+};
+
+__device__ __forceinline__ void group_rows(const RowGroups& g, int e, int& lo, int& hi) {
+    lo = 0;
+    hi = g.n;
+    if (g.offsets) {
+        lo = min(max(g.offsets[e], 0), g.n);
+        hi = max(min(g.offsets[g.whole ? g.groups : e + 1], g.n), lo);
+    }
+}
+
+struct RowTile {
+    int group;       // -1: no such tile
+    int lo, hi;      // its rows
+    int part, parts; // which part of the group's rows this is
+    int index;       // tiles before this group's first one
+};
+
+// Tile number `tile` when every group's rows are cut into tiles of `rows` rows, at least `least` (0 or 1) tiles a group.  All
+// lanes of the wave take part: 64 groups at a time, one scan over the lanes, so up to 64 groups cost one load's latency.
+__device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int least, int tile, int lane) {
+    RowTile t;
+    t.group = -1; t.lo = t.hi = t.part = t.parts = t.index = 0;
+    const int count = g.offsets && !g.whole ? g.groups : 1;
+    int before = 0;
+    for (int base = 0; base < count; base += 64) {
+        const int e = base + lane;
+        int lo = 0, hi = 0, tiles = 0;
+        if (e < count) {
+            group_rows(g, e, lo, hi);
+            tiles = max((hi - lo + rows - 1) / rows, least);
+        }
+        int sum = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(sum, d);
+            if (lane >= d) sum += up;
+        }
+        const uint64_t past = __ballot(before + sum > tile);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            t.group = base + at;
+            lo = __builtin_amdgcn_readlane(lo, at);
+            hi = __builtin_amdgcn_readlane(hi, at);
+            t.parts = __builtin_amdgcn_readlane(tiles, at);
+            t.index = before + __builtin_amdgcn_readlane(sum, at) - t.parts;
+            t.part = tile - t.index;
+            t.lo = min(lo + t.part * rows, hi);
+            t.hi = min(t.lo + rows, hi);
+            return t;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return t;
+}
+
+// The segment a row lies in (the last one that begins at or before it), wave-uniform row; S segments.
+__device__ __forceinline__ int segment_of(const int32_t* __restrict__ offsets, int segments, int row, int lane) {
+    int at = 0;
+    for (int base = 0; base < segments; base += 64) {
+        const int s = base + lane;
+        const bool ended = s < segments && offsets[s + 1] <= row;
+        const int k = __popcll(__ballot(ended));
+        at += k;
+        if (k < 64) break;
+    }
+    return at;
+}
+
+// ---- factors ---------------------------------------------------------------------------------------------------------------
+// A factor is read eight consecutive values at a time (a unit) and becomes kTerms words of eight 16-bit values.
+__device__ __forceinline__ u32x4 zero4() { return u32x4{0u, 0u, 0u, 0u}; }
+
+template <int TERMS>
+__device__ __forceinline__ void split8(f32x8 v, u32x4 (&out)[TERMS]) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        float x0 = v[2 * p], x1 = v[2 * p + 1];
+#pragma unroll
+        for (int term = 0; term < TERMS; ++term) {
+            const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x0, x1}, bf2));
+            out[term][p] = w;
+            x0 -= __builtin_bit_cast(float, w << 16);
+            x1 -= __builtin_bit_cast(float, w & 0xffff0000u);
+        }
+    }
+}
+
+// 16-bit values as they are
+struct Native {
+    struct Raw { u32x4 v; };
+    struct Pointer { const uint16_t* p; int64_t stride; int vec; };
+    static constexpr int kTerms = 1;
+    __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) {
+        Raw r;
+        r.v = zero4();
+        if (valid <= 0) return r;
+        const uint16_t* p = f.p + row * f.stride + col;
+        if (valid >= 8 && f.vec) {
+            r.v = *reinterpret_cast<const u32x4*>(p);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s < valid) r.v[s >> 1] |= (uint32_t)p[s] << (16 * (s & 1));
+        }
+        return r;
+    }
+    __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[1]) { out[0] = r.v; }
+};
+
+// fp32 values as TERMS bf16 terms
+template <int TERMS>
+struct Wide {
+    struct Raw { f32x8 v; };
+    struct Pointer { const float* p; int64_t stride; int vec; };
+    static constexpr int kTerms = TERMS;
+    __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) {
+        Raw r;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) r.v[s] = 0.f;
+        if (valid <= 0) return r;
+        const float* p = f.p + row * f.stride + col;
+        if (valid >= 8 && f.vec) {
+            const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
+            r.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s < valid) r.v[s] = p[s];
+        }
+        return r;
+    }
+    __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[TERMS]) { split8<TERMS>(r.v, out); }
+};
+
+// fp16 values as two bf16 terms (exact)
+struct HalfPair {
+    typedef Native::Raw Raw;
+    typedef Native::Pointer Pointer;
+    static constexpr int kTerms = 2;
+    __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) { return Native::load(f, row, col, valid); }
+    __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[2]) {
+        split8<2>(__builtin_convertvector(__builtin_bit_cast(h8, r.v), f32x8), out);
+    }
+};
+
+__device__ __forceinline__ float signed_byte(uint32_t word, int byte) { return (float)((int)(word << (24 - 8 * byte)) >> 24); }
+
+// 8-bit values with an exponent per 32 of them (neus2_pack8), as bf16 or fp16: q 2^(e-127) has at most 7 significant bits,
+// exact in both.  e = 255 marks a block that held a value that was not finite: 0 * inf = NaN.
+template <bool HALF>
+struct Packed {
+    struct Raw { uint32_t q[2]; uint32_t e; };
+    struct Pointer { const int8_t* p; const uint8_t* e; int64_t stride; };     // stride: 32 * blocks
+    static constexpr int kTerms = 1;
+    __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) {
+        Raw r = {{0u, 0u}, 0u};
+        if (valid <= 0) return r;
+        const int64_t at = row * f.stride + col;                               // behind the last column the packed form holds zeros
+        const uint2 w = *reinterpret_cast<const uint2*>(f.p + at);
+        r.q[0] = w.x;
+        r.q[1] = w.y;
+        r.e = f.e[at >> 5];
+        return r;
+    }
+    __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[1]) {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const float step = __builtin_bit_cast(float, r.e << 23);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const uint32_t w = r.q[p >> 1];
+            const f2 v = {signed_byte(w, 2 * (p & 1)) * step, signed_byte(w, 2 * (p & 1) + 1) * step};
+            out[0][p] = HALF ? __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2)) : __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf2));
+        }
+    }
+};
+
+// ---- tiles -----------------------------------------------------------------------------------------------------------------
+// LINES lines of DEPTH steps of the contraction.  ALONG: the contraction runs along the memory rows (x and W in W x).  Planes of
+// [line][DEPTH], a lane reads its eight steps as one 16-byte piece; piece p of a line lies at p ^ swizzle(line), so that eight
+// consecutive lines of one piece cover every bank once.  Otherwise (ACROSS) every memory row is one step of the contraction;
+// planes of [DEPTH][line], read back transposed by ds_read_b64_tr_b16 (sixteen lanes read four rows of sixteen values, lane c
+// gets column c); piece p of row k lies at p ^ 2 (k % 4), so that the four rows fall on different banks.
+template <class Factor, bool ALONG, int LINES, int DEPTH, int THREADS>
+struct FactorTile {
+    static constexpr int kTerms = Factor::kTerms;
+    static constexpr int kPlane = LINES * DEPTH * 2;
+    static constexpr int kBytes = kPlane * kTerms;
+    static constexpr int kUnits = LINES * DEPTH / 8;
+    static constexpr int kPer = (kUnits + THREADS - 1) / THREADS;
+    static constexpr int kPieces = (ALONG ? DEPTH : LINES) / 8;
+    static_assert(ALONG ? (DEPTH == 32 || DEPTH == 64) : LINES >= 64, "the swizzle needs whole sets of banks");
+    typename Factor::Raw raw[kPer];
+
+    __device__ static __forceinline__ int swizzle(int line) { return DEPTH == 64 ? line & 7 : (line >> 1) & 3; }
+
+    // lines0, step0: where the tile begins; lines, steps: how many there are in all (the rest is zero)
+    __device__ __forceinline__ void load(const typename Factor::Pointer& f, int64_t line0, int lines, int64_t step0, int steps, int tid) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int unit = tid + k * THREADS;
+            const int r = unit / kPieces, c = unit % kPieces * 8;
+            const bool in = kUnits % THREADS == 0 || unit < kUnits;
+            if (ALONG) raw[k] = Factor::load(f, line0 + r, (int)step0 + c, in && r < lines ? steps - c : 0);
+            else raw[k] = Factor::load(f, step0 + r, (int)line0 + c, in && r < steps ? lines - c : 0);
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char* __restrict__ lds, int tid) const {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int unit = tid + k * THREADS;
+            if (kUnits % THREADS != 0 && unit >= kUnits) break;
+            const int r = unit / kPieces, piece = unit % kPieces;
+            u32x4 t[kTerms];
+            Factor::terms(raw[k], t);
+            const int at = r * kPieces * 16 + ((piece ^ (ALONG ? swizzle(r) : (r & 3) << 1)) << 4);
+#pragma unroll
+            for (int term = 0; term < kTerms; ++term) *reinterpret_cast<u32x4*>(lds + term * kPlane + at) = t[term];
+        }
+    }
+    // the operand of k-step ks (16 steps) for the 32 lines from 32 * block on
+    __device__ static __forceinline__ u32x4 operand(const unsigned char* __restrict__ lds, int term, int block, int ks, int lane) {
+        if (ALONG) {
+            const int line = 32 * block + (lane & 31);
+            return *reinterpret_cast<const u32x4*>(lds + term * kPlane + line * (DEPTH * 2) + (((2 * ks + (lane >> 5)) ^ swizzle(line)) << 4));
+        } else {
+            typedef short v4s __attribute__((ext_vector_type(4)));
+            const int quad = (lane >> 2) & 3;
+            const int piece = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+            const unsigned char* at = lds + term * kPlane + (16 * ks + 8 * (lane >> 5) + quad) * (LINES * 2) + ((piece ^ (quad << 1)) << 4) + (lane & 1) * 8;
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at));
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 4 * (LINES * 2)));
+            return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+template <bool HALF>
+__device__ __forceinline__ v16f mma32(const u32x4& a, const u32x4& b, const v16f& c) {
+    if (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+template <bool HALF>
+__device__ __forceinline__ v4f mma16(const u32x4& a, const u32x4& b, const v4f& c) {
+    if (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+// c += the products of the terms of a and b that count: together as far down as the finer factor's last term
+template <bool HALF, int TA, int TB>
+__device__ __forceinline__ v16f mma_terms(const u32x4 (&a)[TA], const u32x4 (&b)[TB], v16f c) {
+    constexpr int kLast = (TA > TB ? TA : TB) - 1;
+#pragma unroll
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+            if (i + j <= kLast) c = mma32<HALF>(a[i], b[j], c);
+    return c;
+}
+
+// ---- conversions to the stored type -------------------------------------------------------------------------------------------
+// four consecutive values of a row; `room`: how many of them lie inside the row; vec: rows begin on multiples of four values
+template <int DT>
+__device__ __forceinline__ void store4(typename TypeOf<DT>::Element* p, const v4f& v, int room, bool vec) {
+    typedef typename TypeOf<DT>::Element E;
+    typedef E E4 __attribute__((ext_vector_type(4)));
+    if (room >= 4 && vec) {
+        *reinterpret_cast<E4*>(p) = __builtin_convertvector(v, E4);        // to the nearest, ties to even
+    } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            if (s < room) p[s] = (E)v[s];
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------------------
+// out[g] (+)= sum over the rows of group g of left_i right_i^T, out [groups][outer][inner] fp32.  left is dy (of the layer's type) or
+// an adapter's v (fp32, dense rows); right is x, x in 8 bits, or an adapter's u.  by_slot: the sums of all segments that share a
+// slot go to that slot's matrix, and slots without rows count as empty groups.
+struct MatrixGradient {
+    RowGroups groups;
+    int dtype;
+    const float* left; const void* dy; int64_t dy_stride;
+    const float* right; const void* x; int64_t x_stride; const int8_t* xq; const uint8_t* xe;
+    int outer, inner;
+    float* out; int accumulate;
+    float* partial;
+    bool by_slot; const int32_t* slots; int n_slots;
+};
+int64_t matrix_gradient_bytes(int groups, int64_t n, int outer, int inner, bool by_slot);
+int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st);
+
+__device__ __forceinline__ int slot_of(const int32_t* __restrict__ slots, int n_slots, int segment) {
+    const int s = slots ? slots[segment] : segment;
+    return s >= 0 && s < n_slots ? s : -1;
+}
+
+inline int element_bytes(int dtype) { return dtype == kTypeF32 ? 4 : 2; }
+
+// rows of `stride` values begin on 16-byte boundaries
+inline int rows_aligned(int dtype, int64_t stride) { return (stride * element_bytes(dtype)) % 16 == 0; }
+
+inline int check_grid(int64_t blocks) {
+    if (blocks > 0x7fffffff) return fail(NEUS2_ERR_SHAPE, "%lld workgroups: too many rows for so many outputs", (long long)blocks);
+    return NEUS2_OK;
+}
+
+// zero below zero, NaN stays NaN
+__device__ __forceinline__ float relu1(float z) { return z <= 0.f ? 0.f : z; }
+
+}  // namespace neus2

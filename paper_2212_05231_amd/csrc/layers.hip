@@ -1,0 +1,764 @@
+// Layers whose rows choose their matrices: forward products and the gradient with respect to the input (one product engine for
+// both), the low-rank part of adapters, and layer inputs in 8 bits.  The gradients of the matrices are in layers_grad.hip.
+#include "layers.h"
+
+namespace neus2 {
+namespace {
+
+struct RowsArgs {
+    RowGroups groups;
+    const void* x; int64_t x_stride; int x_vec;            // the data rows: x forward, dy backward
+    const void* w; int64_t w_group; int w_stride, w_vec;   // matrix of group g at w + g * w_group, memory rows of w_stride values
+    int steps;                                             // length of the contraction
+    int cols;                                              // outputs per row
+    void* y; int64_t y_stride; int y_vec;
+    int relu;
+    const uint32_t* masks; int mask_words;                 // NULL, or: outputs whose bit is not set are zero
+    // adapters: y += bank[slot] u for the rows of each segment
+    const int32_t* segments; int n_segments;
+    const int32_t* slots; int n_slots;
+    const float* u; const void* bank; int rank;
+    int col_tiles;
+};
+
+// The number of bf16 terms an adapter's fp32 u and its bank matrix take in y += bank u.
+template <int DT> struct AdapterTerms {
+    static constexpr int kU = DT == kTypeF32 ? 3 : 2;
+    static constexpr int kBank = DT == kTypeF32 ? 3 : DT == kTypeF16 ? 2 : 1;
+};
+
+// eight values of a row (k .. k + 7 of `rank`) as floats, zero where the row counts for nothing
+__device__ __forceinline__ f32x8 load_u(const float* __restrict__ u, int64_t row, int rank, int k, bool counts) {
+    f32x8 v;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v[s] = 0.f;
+    if (!counts) return v;
+    const float* p = u + row * rank + k;
+    if ((rank & 7) == 0 && k < rank) {
+        const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+        if (k + s < rank) v[s] = p[s];
+    return v;
+}
+
+// eight values bank(col, k .. k + 7): along the memory row forward (bank [col][rank]), down the column backward ([rank][cols])
+template <int DT, bool BACKWARD>
+__device__ __forceinline__ f32x8 load_bank(const typename TypeOf<DT>::Element* __restrict__ bank, int rank, int cols, int col, int k) {
+    f32x8 v;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v[s] = 0.f;
+    if (col >= cols) return v;
+    if (!BACKWARD && (rank & 7) == 0 && k < rank) {
+        typedef typename TypeOf<DT>::Element E;
+        typedef E E4 __attribute__((ext_vector_type(4)));
+        const E* p = bank + (int64_t)col * rank + k;
+        const E4 a = *reinterpret_cast<const E4*>(p), b = *reinterpret_cast<const E4*>(p + 4);
+        return __builtin_convertvector(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), f32x8);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+        if (k + s < rank) v[s] = (float)(BACKWARD ? bank[(int64_t)(k + s) * cols + col] : bank[(int64_t)col * rank + k + s]);
+    return v;
+}
+
+// ---- the product engine ----------------------------------------------------------------------------------------------------
+// One workgroup owns ROWS data rows of one group and COLS outputs; both factors of DEPTH steps of the contraction lie in LDS,
+// fetched into registers while the products of the steps before run.  The matrix's tile is the instruction's first operand, so a
+// lane ends up with four consecutive outputs of one row.
+// BACKWARD = false: y = W x (contraction along the memory rows of W); true: dx = W^T dy (every memory row of W is a step).
+template <int DT, bool BACKWARD, bool ADAPT, int ROWS, int COLS, int WR, int WC, int DEPTH, int BUFS>
+__global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
+    typedef typename TypeOf<DT>::Element E;
+    typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
+    constexpr int kThreads = 64 * WR * WC;
+    constexpr int kBR = ROWS / WR / 32, kBC = COLS / WC / 32, kTerms = Factor::kTerms;
+    constexpr bool kHalf = DT == kTypeF16;
+    typedef FactorTile<Factor, true, ROWS, DEPTH, kThreads> DataTile;
+    typedef FactorTile<Factor, !BACKWARD, COLS, DEPTH, kThreads> MatrixTile;
+    constexpr int kBuf = DataTile::kBytes + MatrixTile::kBytes;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[BUFS * kBuf];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave / WC, wc = wave % WC;
+    const int col0 = (int)(blockIdx.x % a.col_tiles) * COLS;
+    const RowTile t = locate(a.groups, ROWS, 0, (int)(blockIdx.x / a.col_tiles), lane);
+    if (t.group < 0) return;
+
+    typename Factor::Pointer data, matrix;
+    data.p = reinterpret_cast<decltype(data.p)>(a.x);
+    data.stride = a.x_stride;
+    data.vec = a.x_vec;
+    matrix.p = reinterpret_cast<decltype(matrix.p)>(a.w) + (int64_t)t.group * a.w_group;
+    matrix.stride = a.w_stride;
+    matrix.vec = a.w_vec;
+    DataTile dt;
+    MatrixTile mt;
+    v16f acc[kBC][kBR];
+#pragma unroll
+    for (int c = 0; c < kBC; ++c)
+#pragma unroll
+        for (int r = 0; r < kBR; ++r) acc[c][r] = zero16();
+
+    const int rounds = (a.steps + DEPTH - 1) / DEPTH;
+    dt.load(data, t.lo, t.hi - t.lo, 0, a.steps, tid);
+    mt.load(matrix, col0, a.cols - col0, 0, a.steps, tid);
+    dt.store(lds, tid);
+    mt.store(lds + DataTile::kBytes, tid);
+    __syncthreads();
+    for (int k = 0; k < rounds; ++k) {
+        const unsigned char* buf = lds + (BUFS == 2 ? (k & 1) * kBuf : 0);
+        const bool more = k + 1 < rounds;
+        if (more) {
+            const int step = (k + 1) * DEPTH;
+            dt.load(data, t.lo, t.hi - t.lo, step, a.steps - step, tid);
+            mt.load(matrix, col0, a.cols - col0, step, a.steps - step, tid);
+        }
+#pragma unroll
+        for (int ks = 0; ks < DEPTH / 16; ++ks) {
+            u32x4 m[kBC][kTerms], d[kBR][kTerms];
+#pragma unroll
+            for (int c = 0; c < kBC; ++c)
+#pragma unroll
+                for (int p = 0; p < kTerms; ++p) m[c][p] = MatrixTile::operand(buf + DataTile::kBytes, p, wc * kBC + c, ks, lane);
+#pragma unroll
+            for (int r = 0; r < kBR; ++r)
+#pragma unroll
+                for (int p = 0; p < kTerms; ++p) d[r][p] = DataTile::operand(buf, p, wr * kBR + r, ks, lane);
+#pragma unroll
+            for (int c = 0; c < kBC; ++c)
+#pragma unroll
+                for (int r = 0; r < kBR; ++r) acc[c][r] = mma_terms<kHalf>(m[c], d[r], acc[c][r]);
+        }
+        if (BUFS == 1) __syncthreads();
+        if (more) {
+            unsigned char* next = lds + (BUFS == 2 ? ((k + 1) & 1) * kBuf : 0);
+            dt.store(next, tid);
+            mt.store(next + DataTile::kBytes, tid);
+        }
+        __syncthreads();
+    }
+
+    const int j = lane & 31, h = lane >> 5;
+    if (ADAPT) {
+        // y += bank[slot] u, segment after segment: operands straight from memory (a lane's eight values lie together), the rows of
+        // other segments zero.  A tile inside one segment takes rank / 16 more k-steps.
+        constexpr int kU = AdapterTerms<DT>::kU, kBank = AdapterTerms<DT>::kBank;
+        int s = segment_of(a.segments, a.n_segments, t.lo, lane);
+        for (; s < a.n_segments; ++s) {
+            const int lo = max(a.segments[s], t.lo), hi = min(a.segments[s + 1], t.hi);
+            if (lo >= t.hi) break;
+            const int slot = hi > lo ? slot_of(a.slots, a.n_slots, s) : -1;
+            if (slot < 0) continue;
+            const E* bank = reinterpret_cast<const E*>(a.bank) + (int64_t)slot * a.rank * a.cols;
+            for (int k0 = 0; k0 < a.rank; k0 += 16) {
+                u32x4 b[kBC][kBank];
+#pragma unroll
+                for (int c = 0; c < kBC; ++c)
+                    split8<kBank>(load_bank<DT, BACKWARD>(bank, a.rank, a.cols, col0 + 32 * (wc * kBC + c) + j, k0 + 8 * h), b[c]);
+#pragma unroll
+                for (int r = 0; r < kBR; ++r) {
+                    const int first = t.lo + 32 * (wr * kBR + r), row = first + j;
+                    if (first >= hi || first + 32 <= lo) continue;
+                    u32x4 u[kU];
+                    split8<kU>(load_u(a.u, row, a.rank, k0 + 8 * h, row >= lo && row < hi), u);
+#pragma unroll
+                    for (int c = 0; c < kBC; ++c) acc[c][r] = mma_terms<false>(b[c], u, acc[c][r]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kBR; ++r) {
+        const int row = t.lo + 32 * (wr * kBR + r) + j;
+        if (row >= t.hi) continue;
+        E* out = reinterpret_cast<E*>(a.y) + (int64_t)row * a.y_stride;
+#pragma unroll
+        for (int c = 0; c < kBC; ++c) {
+            const int block = col0 + 32 * (wc * kBC + c);
+            if (block >= a.cols) continue;
+            const uint32_t mask = a.masks ? a.masks[(int64_t)row * a.mask_words + (block >> 5)] : 0xffffffffu;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = block + 8 * g + 4 * h;
+                v4f v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float z = acc[c][r][4 * g + e];
+                    v[e] = (mask >> (8 * g + 4 * h + e)) & 1u ? (a.relu ? relu1(z) : z) : 0.f;
+                }
+                store4<DT>(out + col, v, a.cols - col, a.y_vec);
+            }
+        }
+    }
+}
+
+// ---- few rows ------------------------------------------------------------------------------------------------------------------
+// 16 rows and 16 outputs on the 16x16x32 instruction, operands straight from memory: with so few rows the pass is bound by reading
+// the matrices once, and there is nothing to share through LDS.  A lane reads 32 consecutive bytes of a matrix row, four lanes a
+// whole line.  SPLIT: the four waves of a workgroup share the contraction (their sums are joined in LDS); otherwise every wave has 16
+// rows of its own.  TO_U: the low-rank products u = scale A x and v = scale B^T dy of adapters, in fp32, every segment with the
+// matrix of its slot (rows of a segment without one get zeros).  DOWN: the contraction runs down the matrix's columns (B^T dy).
+struct FewArgs {
+    RowGroups groups;
+    const void* x; int64_t x_stride; int x_vec;
+    const void* w; int64_t w_group; int w_stride, w_vec;
+    int steps, cols;
+    void* y; int64_t y_stride;
+    int relu;
+    const int32_t* slots; int n_slots; const float* scales;       // TO_U
+    const int32_t* segments; int n_segments;                      // !TO_U with adapters
+    const float* u; const void* bank; int rank;
+    int col_tiles;
+};
+
+template <int DT, bool TO_U, bool DOWN, bool SPLIT>
+__global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a) {
+    typedef typename TypeOf<DT>::Element E;
+    typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
+    constexpr int kTerms = Factor::kTerms;
+    constexpr bool kHalf = DT == kTypeF16;
+    constexpr int kUnits = DT == kTypeF32 ? 1 : 2;            // operands a lane takes of one line of 128 bytes
+    constexpr int kChunk = 32 * kUnits;                       // steps of the contraction they cover
+    constexpr int kAhead = 4;
+    constexpr int kRows = SPLIT ? 16 : 64;
+    __shared__ v4f part[SPLIT ? 4 : 1][64];
+    __shared__ int row_slot[16];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col0 = (int)(blockIdx.x % a.col_tiles) * 16;
+    RowTile t = locate(a.groups, kRows, 0, (int)(blockIdx.x / a.col_tiles), lane);
+    if (t.group < 0) return;
+    if (!SPLIT) {
+        t.lo += 16 * wave;
+        if (t.lo >= t.hi) return;
+    }
+    int slot = t.group;
+    if (TO_U) slot = slot_of(a.slots, a.n_slots, t.group);
+
+    const int i = lane & 15, quarter = lane >> 4;
+    v4f acc = {0.f, 0.f, 0.f, 0.f};
+    if (slot >= 0) {
+        typename Factor::Pointer data, matrix;
+        data.p = reinterpret_cast<decltype(data.p)>(a.x);
+        data.stride = a.x_stride;
+        data.vec = a.x_vec;
+        matrix.p = reinterpret_cast<decltype(matrix.p)>(a.w) + (int64_t)slot * a.w_group;
+        matrix.stride = a.w_stride;
+        matrix.vec = a.w_vec;
+        const bool row_in = t.lo + i < t.hi, col_in = col0 + i < a.cols;
+        const int stride = (SPLIT ? 4 : 1) * kChunk;
+        for (int base = SPLIT ? wave * kChunk : 0; base < a.steps; base += kAhead * stride) {
+            typename Factor::Raw w[kAhead][kUnits], x[kAhead][kUnits];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int v = 0; v < kUnits; ++v) {
+                    const int k = base + q * stride + 8 * kUnits * quarter + 8 * v;
+                    if (DOWN) {
+                        typename Factor::Raw& r = w[q][v];
+                        r.v = Factor::load(matrix, 0, 0, 0).v;
+                        const E* p = reinterpret_cast<const E*>(matrix.p) + (int64_t)k * a.w_stride + col0 + i;
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            if (col_in && k + s < a.steps) {
+                                const E value = p[(int64_t)s * a.w_stride];
+                                if constexpr (DT == kTypeF32) r.v[s] = value;
+                                else r.v[s >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, value) << (16 * (s & 1));
+                            }
+                    } else {
+                        w[q][v] = Factor::load(matrix, col0 + i, k, col_in ? a.steps - k : 0);
+                    }
+                    x[q][v] = Factor::load(data, t.lo + i, k, row_in ? a.steps - k : 0);
+                }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int v = 0; v < kUnits; ++v) {
+                    u32x4 wt[kTerms], xt[kTerms];
+                    Factor::terms(w[q][v], wt);
+                    Factor::terms(x[q][v], xt);
+#pragma unroll
+                    for (int p = 0; p < kTerms; ++p)
+#pragma unroll
+                        for (int r = 0; r < kTerms; ++r)
+                            if (p + r < kTerms) acc = mma16<kHalf>(wt[p], xt[r], acc);
+                }
+        }
+    }
+    // lane: row lane % 16, outputs 4 (lane / 16) .. + 3
+    if constexpr (SPLIT) {
+        if (!TO_U && a.rank > 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = min(t.lo + 4 * wave + r, t.hi - 1);
+                const int s = segment_of(a.segments, a.n_segments, row, lane);
+                const int of = s < a.n_segments ? slot_of(a.slots, a.n_slots, s) : -1;
+                if (lane == 0) row_slot[4 * wave + r] = of;
+            }
+        }
+        part[wave][lane] = acc;
+        __syncthreads();
+        // a thread per output, the outputs of a row side by side
+        const int row = tid >> 4, c = tid & 15, col = col0 + c;
+        float z = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) z += part[w][(c >> 2) * 16 + row][c & 3];
+        const int64_t at = t.lo + row;
+        if (at >= t.hi || col >= a.cols) return;
+        if constexpr (TO_U) {
+            reinterpret_cast<float*>(a.y)[at * a.y_stride + col] = slot >= 0 ? z * a.scales[slot] : 0.f;
+        } else {
+            if (a.rank > 0 && row_slot[row] >= 0) {
+                const E* bank = reinterpret_cast<const E*>(a.bank) + (int64_t)row_slot[row] * a.rank * a.cols;
+                for (int k = 0; k < a.rank; k += 8) {
+                    const f32x8 b = load_bank<DT, false>(bank, a.rank, a.cols, col, k), u = load_u(a.u, at, a.rank, k, true);
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) z += b[s] * u[s];
+                }
+            }
+            reinterpret_cast<E*>(a.y)[at * a.y_stride + col] = (E)(a.relu ? relu1(z) : z);
+        }
+    } else {
+        static_assert(SPLIT || TO_U, "rows of their own: the low-rank products only");
+        const int64_t at = t.lo + i;
+        if (at >= t.hi) return;
+        const float scale = slot >= 0 ? a.scales[slot] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int col = col0 + 4 * quarter + e;
+            if (col < a.cols) reinterpret_cast<float*>(a.y)[at * a.y_stride + col] = slot >= 0 ? acc[e] * scale : 0.f;
+        }
+    }
+}
+
+// ---- layer inputs in 8 bits -------------------------------------------------------------------------------------------------------
+// A thread has eight features of a row, four threads a block of 32: its largest magnitude decides the exponent, the smallest t at
+// which it rounds to at most 127 steps of 2^t (t >= -126).  All of it is exact: x 2^-t is a change of exponent, the rounding to whole
+// steps (ties to even) the only one.  Bound by the memory: 4 or 2 bytes read, 1.03 (1.16 with masks) written a feature.
+template <int DT>
+__global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ x, int64_t x_stride, int vec, int64_t n, int dim,
+                                                   int8_t* __restrict__ q, uint8_t* __restrict__ e, uint32_t* __restrict__ masks) {
+    typedef std::conditional_t<DT == kTypeF32, Wide<1>, Native> Factor;
+    const int units = (dim + 31) / 32 * 4;
+    const int64_t total = n * units, step = (int64_t)gridDim.x * 256;
+    typename Factor::Pointer f;
+    f.p = reinterpret_cast<decltype(f.p)>(x);
+    f.stride = x_stride;
+    f.vec = vec;
+    for (int64_t base = (int64_t)blockIdx.x * 256; base < total; base += step) {
+        const int64_t at = base + threadIdx.x;
+        if (at >= total) break;                                            // whole groups of four lanes leave together
+        const int64_t row = at / units;
+        const int unit = (int)(at - row * units);
+        const typename Factor::Raw raw = Factor::load(f, row, 8 * unit, dim - 8 * unit);
+        f32x8 v;
+        if constexpr (DT == kTypeF32) v = raw.v;
+        else if constexpr (DT == kTypeF16) v = __builtin_convertvector(__builtin_bit_cast(h8, raw.v), f32x8);
+        else v = __builtin_convertvector(__builtin_bit_cast(bf8, raw.v), f32x8);
+        // magnitudes as bit patterns: their order is the numbers', infinities and NaN on top
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float vs = v[s];
+            top = max(top, __builtin_bit_cast(uint32_t, vs) & 0x7fffffffu);
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+        const bool finite = top < 0x7f800000u;
+        const int biased = max((int)(top >> 23) - 6 + ((top & 0x7fffffu) >= 0x7f0000u ? 1 : 0), 1);     // t + 127
+        const float inverse = __builtin_bit_cast(float, (uint32_t)(254 - min(biased, 253)) << 23);
+        // where the 64th step is beyond the type's largest number
+        const float most = biased == (DT == kTypeF16 ? 137 : 249) ? 63.f : 127.f;
+        uint32_t bits = 0, word[2] = {0u, 0u};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float vs = v[s];
+            bits |= (vs > 0.f ? 1u : 0u) << s;
+            const float steps = fminf(fmaxf(__builtin_rintf(vs * inverse), -most), most);
+            word[s >> 2] |= ((uint32_t)(int)(finite ? steps : 0.f) & 0xffu) << (8 * (s & 3));
+        }
+        const int64_t block = at >> 2;
+        if (q) *reinterpret_cast<uint2*>(q + 8 * at) = make_uint2(word[0], word[1]);
+        if (q && (unit & 3) == 0) e[block] = (uint8_t)(finite ? biased : 255);
+        if (masks) {
+            bits <<= 8 * (unit & 3);
+            bits |= (uint32_t)__shfl_xor((int)bits, 1);
+            bits |= (uint32_t)__shfl_xor((int)bits, 2);
+            if ((unit & 3) == 0) masks[block] = bits;
+        }
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int64_t n, int dim,
+                                                     void* __restrict__ x, int64_t x_stride, int vec) {
+    typedef typename TypeOf<DT>::Element E;
+    typedef E E8 __attribute__((ext_vector_type(8)));
+    const int units = (dim + 31) / 32 * 4;
+    const int64_t total = n * units, step = (int64_t)gridDim.x * 256;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += step) {
+        const int64_t row = at / units;
+        const int col = 8 * (int)(at - row * units), room = dim - col;
+        if (room <= 0) continue;
+        const uint2 w = *reinterpret_cast<const uint2*>(q + 8 * at);
+        const float scale = __builtin_bit_cast(float, (uint32_t)e[at >> 2] << 23);
+        f32x8 v;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) v[s] = signed_byte(s < 4 ? w.x : w.y, s & 3) * scale;
+        E* p = reinterpret_cast<E*>(x) + row * x_stride + col;
+        if (room >= 8 && vec) {
+            *reinterpret_cast<E8*>(p) = __builtin_convertvector(v, E8);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s < room) p[s] = (E)v[s];
+        }
+    }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------------------
+int64_t row_tiles(const RowGroups& g, int rows) {
+    return ((int64_t)g.n + rows - 1) / rows + (g.offsets && !g.whole ? g.groups : 0);
+}
+
+template <int DT, bool BACKWARD, bool ADAPT>
+int launch_rows(RowsArgs a, hipStream_t st) {
+    constexpr int kDepth = DT == kTypeF32 ? 32 : 64, kBufs = DT == kTypeF32 ? 1 : 2;
+    if (a.cols > 64) {
+        a.col_tiles = (a.cols + 127) / 128;
+        NEUS2_TRY(check_grid(row_tiles(a.groups, 128) * a.col_tiles));
+        rows_kernel<DT, BACKWARD, ADAPT, 128, 128, 2, 2, kDepth, kBufs><<<dim3((unsigned)(row_tiles(a.groups, 128) * a.col_tiles)), 256, 0, st>>>(a);
+    } else {
+        a.col_tiles = 1;
+        rows_kernel<DT, BACKWARD, ADAPT, 128, 64, 4, 1, kDepth, kBufs><<<dim3((unsigned)row_tiles(a.groups, 128)), 256, 0, st>>>(a);
+    }
+    return check_launch(BACKWARD ? "layer backward" : "layer forward");
+}
+
+template <bool BACKWARD>
+int launch_rows(int dtype, const RowsArgs& a, hipStream_t st) {
+    if (a.rank > 0) {
+        if (dtype == kTypeF32) return launch_rows<kTypeF32, BACKWARD, true>(a, st);
+        if (dtype == kTypeF16) return launch_rows<kTypeF16, BACKWARD, true>(a, st);
+        return launch_rows<kTypeBF16, BACKWARD, true>(a, st);
+    }
+    if (dtype == kTypeF32) return launch_rows<kTypeF32, BACKWARD, false>(a, st);
+    if (dtype == kTypeF16) return launch_rows<kTypeF16, BACKWARD, false>(a, st);
+    return launch_rows<kTypeBF16, BACKWARD, false>(a, st);
+}
+
+template <bool TO_U, bool DOWN, bool SPLIT>
+int launch_few(int dtype, FewArgs a, hipStream_t st) {
+    a.col_tiles = (a.cols + 15) / 16;
+    const int64_t blocks = row_tiles(a.groups, SPLIT ? 16 : 64) * a.col_tiles;
+    NEUS2_TRY(check_grid(blocks));
+    const dim3 grid((unsigned)blocks);
+    if (dtype == kTypeF32) few_rows_kernel<kTypeF32, TO_U, DOWN, SPLIT><<<grid, 256, 0, st>>>(a);
+    else if (dtype == kTypeF16) few_rows_kernel<kTypeF16, TO_U, DOWN, SPLIT><<<grid, 256, 0, st>>>(a);
+    else few_rows_kernel<kTypeBF16, TO_U, DOWN, SPLIT><<<grid, 256, 0, st>>>(a);
+    return check_launch("layer, few rows");
+}
+
+RowGroups make_groups(const int32_t* offsets, int groups, int64_t n, bool whole) {
+    RowGroups g;
+    g.offsets = offsets;
+    g.groups = groups;
+    g.n = (int32_t)n;
+    g.whole = whole ? 1 : 0;
+    return g;
+}
+
+// u = scale A[slot] x (DOWN = false: matrices [slots][rank][steps]) or v = scale B[slot]^T dy (DOWN = true: [slots][steps][rank])
+template <bool DOWN>
+int launch_low_rank(const neus2_layer* l, const void* x, int64_t x_stride, const void* bank, const float* scales, const int32_t* slots,
+                    const int32_t* offsets, int64_t n, int steps, float* u, hipStream_t st) {
+    FewArgs a = {};
+    a.groups = make_groups(offsets, l->groups, n, false);
+    a.x = x;
+    a.x_stride = x_stride;
+    a.x_vec = rows_aligned(l->dtype, x_stride);
+    a.w = bank;
+    a.w_group = (int64_t)l->rank * steps;
+    a.w_stride = DOWN ? l->rank : steps;
+    a.w_vec = rows_aligned(l->dtype, steps);
+    a.steps = steps;
+    a.cols = l->rank;
+    a.y = u;
+    a.y_stride = l->rank;
+    a.slots = slots;
+    a.n_slots = l->adapters;
+    a.scales = scales;
+    return steps > 256 ? launch_few<true, DOWN, true>(l->dtype, a, st) : launch_few<true, DOWN, false>(l->dtype, a, st);
+}
+
+// ---- argument checks ------------------------------------------------------------------------------------------------------------------
+int64_t x_stride_of(const neus2_layer* l) { return l->x_stride ? l->x_stride : l->in_dim; }
+int64_t y_stride_of(const neus2_layer* l) { return l->y_stride ? l->y_stride : l->out_dim; }
+
+int check_layer(const neus2_layer* l, bool adapters) {
+    if (!l) return fail(NEUS2_ERR_NULL, "layer is NULL");
+    if (l->dtype < 0 || l->dtype > 2) return fail(NEUS2_ERR_CONFIG, "dtype = %d, must be 0 (fp32), 1 (fp16) or 2 (bf16)", l->dtype);
+    if (l->groups < 1 || l->groups > (1 << 20)) return fail(NEUS2_ERR_CONFIG, "groups = %d, must be 1..2^20", l->groups);
+    if (l->in_dim < 1 || l->in_dim > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "in_dim = %d, must be 1..65536", l->in_dim);
+    if (l->out_dim < 1 || l->out_dim > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "out_dim = %d, must be 1..65536", l->out_dim);
+    if (l->x_stride != 0 && (l->x_stride < l->in_dim || l->x_stride > (1 << 24)))
+        return fail(NEUS2_ERR_SHAPE, "x_stride = %lld, must be 0 or in_dim..2^24", (long long)l->x_stride);
+    if (l->y_stride != 0 && (l->y_stride < l->out_dim || l->y_stride > (1 << 24)))
+        return fail(NEUS2_ERR_SHAPE, "y_stride = %lld, must be 0 or out_dim..2^24", (long long)l->y_stride);
+    if (l->relu != 0 && l->relu != 1) return fail(NEUS2_ERR_CONFIG, "relu = %d, must be 0 or 1", l->relu);
+    if (l->accumulate != 0 && l->accumulate != 1) return fail(NEUS2_ERR_CONFIG, "accumulate = %d, must be 0 or 1", l->accumulate);
+    if (adapters) {
+        if (l->rank < 1 || l->rank > 64) return fail(NEUS2_ERR_UNSUPPORTED, "rank = %d, kernels exist for 1..64", l->rank);
+        if (l->adapters < 1 || l->adapters > (1 << 20)) return fail(NEUS2_ERR_CONFIG, "adapters = %d, must be 1..2^20", l->adapters);
+    } else if (l->rank != 0 || l->adapters != 0) {
+        return fail(NEUS2_ERR_CONFIG, "rank = %d, adapters = %d: a grouped layer has no adapters", l->rank, l->adapters);
+    }
+    return NEUS2_OK;
+}
+
+int check_input(const void* x, const int8_t* xq, const uint8_t* xe, int64_t n) {
+    if (x && (xq || xe)) return fail(NEUS2_ERR_CONFIG, "x and xq given: the layer's input is one or the other");
+    if (xq || xe) {
+        NEUS2_TRY(check_ptr(xq, "xq"));
+        return check_ptr(xe, "xe");
+    }
+    return check_ptr(x, "x", n > 0);
+}
+
+}  // namespace
+}  // namespace neus2
+
+using namespace neus2;
+
+extern "C" {
+
+int neus2_grouped_fwd(const neus2_layer* l, const void* x, const void* W, const int32_t* offsets, int64_t n, void* y, void* stream) {
+    NEUS2_TRY(check_layer(l, false));
+    NEUS2_TRY(check_count(n, "n"));
+    NEUS2_TRY(check_ptr(x, "x", n > 0));
+    NEUS2_TRY(check_ptr(W, "W"));
+    NEUS2_TRY(check_ptr(offsets, "offsets", l->groups > 1));
+    NEUS2_TRY(check_ptr(y, "y", n > 0));
+    if (n == 0) return NEUS2_OK;
+    hipStream_t st = (hipStream_t)stream;
+    const RowGroups groups = make_groups(offsets, l->groups, n, false);
+    if (n <= 16 * (int64_t)l->groups) {                       // 16 rows a group and fewer: the matrices are read once, and little else
+        FewArgs a = {};
+        a.groups = groups;
+        a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
+        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
+        a.steps = l->in_dim; a.cols = l->out_dim;
+        a.y = y; a.y_stride = y_stride_of(l);
+        a.relu = l->relu;
+        return launch_few<false, false, true>(l->dtype, a, st);
+    }
+    RowsArgs a = {};
+    a.groups = groups;
+    a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
+    a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
+    a.steps = l->in_dim; a.cols = l->out_dim;
+    a.y = y; a.y_stride = y_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+    a.relu = l->relu;
+    return launch_rows<false>(l->dtype, a, st);
+}
+
+int64_t neus2_grouped_workspace_bytes(const neus2_layer* l, int64_t n) {
+    if (check_layer(l, false) != NEUS2_OK || check_count(n, "n") != NEUS2_OK) return -1;
+    return matrix_gradient_bytes(l->groups, n, l->out_dim, l->in_dim, false);
+}
+
+int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, const uint8_t* xe, const uint32_t* masks, const void* W,
+                      const int32_t* offsets, const void* dy, int64_t n, void* dx, float* dW, void* workspace, int64_t workspace_bytes,
+                      void* stream) {
+    NEUS2_TRY(check_layer(l, false));
+    NEUS2_TRY(check_count(n, "n"));
+    if (!dx && !dW && n > 0) return fail(NEUS2_ERR_NULL, "dx and dW are NULL: nothing to compute");
+    if (dW) NEUS2_TRY(check_input(x, xq, xe, n));
+    if (dx && n > 0) NEUS2_TRY(check_ptr(W, "W"));
+    NEUS2_TRY(check_ptr(masks, "masks", false));
+    NEUS2_TRY(check_ptr(offsets, "offsets", l->groups > 1));
+    NEUS2_TRY(check_ptr(dy, "dy", n > 0));
+    NEUS2_TRY(check_ptr(dx, "dx", false));
+    NEUS2_TRY(check_ptr(dW, "dW", false));
+    NEUS2_TRY(check_ptr(workspace, "workspace", false));
+    const int64_t need = dW ? matrix_gradient_bytes(l->groups, n, l->out_dim, l->in_dim, false) : 0;
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(NEUS2_ERR_SHAPE, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)need);
+    hipStream_t st = (hipStream_t)stream;
+    if (dx && n > 0) {
+        RowsArgs a = {};
+        a.groups = make_groups(offsets, l->groups, n, false);
+        a.x = dy; a.x_stride = y_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
+        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
+        a.steps = l->out_dim; a.cols = l->in_dim;
+        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+        a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
+        NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
+    }
+    if (!dW) return NEUS2_OK;
+    MatrixGradient m = {};
+    m.groups = make_groups(offsets, l->groups, n, false);
+    m.dtype = l->dtype;
+    m.dy = dy; m.dy_stride = y_stride_of(l);
+    m.x = x; m.x_stride = x_stride_of(l); m.xq = xq; m.xe = xe;
+    m.outer = l->out_dim; m.inner = l->in_dim;
+    m.out = dW; m.accumulate = l->accumulate;
+    m.partial = (float*)workspace;
+    return launch_matrix_gradient(m, st);
+}
+
+int neus2_adapter_fwd(const neus2_layer* l, const void* x, const void* W, const void* A, const void* B, const float* scales,
+                      const int32_t* slots, const int32_t* offsets, int64_t n, float* u, void* y, void* stream) {
+    NEUS2_TRY(check_layer(l, true));
+    NEUS2_TRY(check_count(n, "n"));
+    NEUS2_TRY(check_ptr(x, "x", n > 0));
+    NEUS2_TRY(check_ptr(W, "W"));
+    NEUS2_TRY(check_ptr(A, "A"));
+    NEUS2_TRY(check_ptr(B, "B"));
+    NEUS2_TRY(check_ptr(scales, "scales"));
+    NEUS2_TRY(check_ptr(slots, "slots", false));
+    NEUS2_TRY(check_ptr(offsets, "offsets"));
+    NEUS2_TRY(check_ptr(u, "u", n > 0));
+    NEUS2_TRY(check_ptr(y, "y", n > 0));
+    if (n == 0) return NEUS2_OK;
+    hipStream_t st = (hipStream_t)stream;
+    NEUS2_TRY(launch_low_rank<false>(l, x, x_stride_of(l), A, scales, slots, offsets, n, l->in_dim, u, st));
+    const RowGroups whole = make_groups(offsets, l->groups, n, true);
+    if (n <= 64) {
+        FewArgs a = {};
+        a.groups = whole;
+        a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
+        a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
+        a.steps = l->in_dim; a.cols = l->out_dim;
+        a.y = y; a.y_stride = y_stride_of(l);
+        a.relu = l->relu;
+        a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
+        a.u = u; a.bank = B; a.rank = l->rank;
+        return launch_few<false, false, true>(l->dtype, a, st);
+    }
+    RowsArgs a = {};
+    a.groups = whole;
+    a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
+    a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
+    a.steps = l->in_dim; a.cols = l->out_dim;
+    a.y = y; a.y_stride = y_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+    a.relu = l->relu;
+    a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
+    a.u = u; a.bank = B; a.rank = l->rank;
+    return launch_rows<false>(l->dtype, a, st);
+}
+
+int64_t neus2_adapter_workspace_bytes(const neus2_layer* l, int64_t n) {
+    if (check_layer(l, true) != NEUS2_OK || check_count(n, "n") != NEUS2_OK) return -1;
+    const int64_t v = (n * l->rank * 4 + 15) / 16 * 16;
+    const int64_t da = matrix_gradient_bytes(l->groups, n, l->rank, l->in_dim, true);
+    const int64_t db = matrix_gradient_bytes(l->groups, n, l->out_dim, l->rank, true);
+    return v + (da > db ? da : db);
+}
+
+int neus2_adapter_bwd(const neus2_layer* l, const void* x, const int8_t* xq, const uint8_t* xe, const uint32_t* masks, const void* W,
+                      const void* A, const void* B, const float* scales, const int32_t* slots, const int32_t* offsets, const float* u,
+                      const void* dy, int64_t n, void* dx, float* dA, float* dB, void* workspace, int64_t workspace_bytes, void* stream) {
+    NEUS2_TRY(check_layer(l, true));
+    NEUS2_TRY(check_count(n, "n"));
+    if ((dA == nullptr) != (dB == nullptr)) return fail(NEUS2_ERR_NULL, "dA and dB: both or neither");
+    if (!dx && !dA && n > 0) return fail(NEUS2_ERR_NULL, "dx, dA and dB are NULL: nothing to compute");
+    if (dA) NEUS2_TRY(check_input(x, xq, xe, n));
+    if (dx && n > 0) NEUS2_TRY(check_ptr(W, "W"));
+    if (dx && n > 0) NEUS2_TRY(check_ptr(A, "A"));
+    NEUS2_TRY(check_ptr(B, "B"));
+    NEUS2_TRY(check_ptr(masks, "masks", false));
+    NEUS2_TRY(check_ptr(scales, "scales"));
+    NEUS2_TRY(check_ptr(slots, "slots", false));
+    NEUS2_TRY(check_ptr(offsets, "offsets"));
+    if (dB) NEUS2_TRY(check_ptr(u, "u", n > 0));
+    NEUS2_TRY(check_ptr(dy, "dy", n > 0));
+    NEUS2_TRY(check_ptr(dx, "dx", false));
+    NEUS2_TRY(check_ptr(dA, "dA", false));
+    NEUS2_TRY(check_ptr(dB, "dB", false));
+    NEUS2_TRY(check_ptr(workspace, "workspace", n > 0 || dA));
+    const int64_t need = neus2_adapter_workspace_bytes(l, n);
+    if (workspace_bytes < need)
+        return fail(NEUS2_ERR_SHAPE, "workspace of %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+    hipStream_t st = (hipStream_t)stream;
+    float* v = (float*)workspace;
+    float* partial = v + (n * l->rank * 4 + 15) / 16 * 4;
+    if (n > 0) NEUS2_TRY(launch_low_rank<true>(l, dy, y_stride_of(l), B, scales, slots, offsets, n, l->out_dim, v, st));
+    if (dx && n > 0) {
+        RowsArgs a = {};
+        a.groups = make_groups(offsets, l->groups, n, true);
+        a.x = dy; a.x_stride = y_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
+        a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
+        a.steps = l->out_dim; a.cols = l->in_dim;
+        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+        a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
+        a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
+        a.u = v; a.bank = A; a.rank = l->rank;
+        NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
+    }
+    if (!dA) return NEUS2_OK;
+    MatrixGradient m = {};
+    m.groups = make_groups(offsets, l->groups, n, false);
+    m.dtype = l->dtype;
+    m.by_slot = true; m.slots = slots; m.n_slots = l->adapters;
+    m.accumulate = l->accumulate;
+    m.partial = partial;
+    m.outer = l->rank; m.inner = l->in_dim;                    // dA[slot] = sum v x^T
+    m.left = v;
+    m.x = x; m.x_stride = x_stride_of(l); m.xq = xq; m.xe = xe;
+    m.out = dA;
+    NEUS2_TRY(launch_matrix_gradient(m, st));
+    m.outer = l->out_dim; m.inner = l->rank;                   // dB[slot] = sum dy u^T
+    m.left = nullptr; m.dy = dy; m.dy_stride = y_stride_of(l);
+    m.right = u; m.x = nullptr; m.xq = nullptr; m.xe = nullptr;
+    m.out = dB;
+    return launch_matrix_gradient(m, st);
+}
+
+static int check_pack(int dtype, int64_t n, int32_t dim, int64_t x_stride) {
+    if (dtype < 0 || dtype > 2) return fail(NEUS2_ERR_CONFIG, "dtype = %d, must be 0 (fp32), 1 (fp16) or 2 (bf16)", dtype);
+    NEUS2_TRY(check_count(n, "n"));
+    if (dim < 1 || dim > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "dim = %d, must be 1..65536", dim);
+    if (x_stride != 0 && (x_stride < dim || x_stride > (1 << 24)))
+        return fail(NEUS2_ERR_SHAPE, "x_stride = %lld, must be 0 or dim..2^24", (long long)x_stride);
+    return NEUS2_OK;
+}
+
+int neus2_pack8(int32_t dtype, const void* x, int64_t x_stride, int64_t n, int32_t dim, int8_t* q, uint8_t* e, uint32_t* masks, void* stream) {
+    NEUS2_TRY(check_pack(dtype, n, dim, x_stride));
+    NEUS2_TRY(check_ptr(x, "x", n > 0));
+    const bool masks_only = masks && !q && !e;
+    NEUS2_TRY(check_ptr(q, "q", n > 0 && !masks_only));
+    NEUS2_TRY(check_ptr(e, "e", n > 0 && !masks_only));
+    NEUS2_TRY(check_ptr(masks, "masks", false));
+    if (n == 0) return NEUS2_OK;
+    hipStream_t st = (hipStream_t)stream;
+    const int64_t stride = x_stride ? x_stride : dim, blocks = (n * ((dim + 31) / 32 * 4) + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 8 * compute_units() ? blocks : 8 * compute_units());
+    const int vec = rows_aligned(dtype, stride);
+    if (dtype == kTypeF32) pack_kernel<kTypeF32><<<grid, 256, 0, st>>>(x, stride, vec, n, dim, q, e, masks);
+    else if (dtype == kTypeF16) pack_kernel<kTypeF16><<<grid, 256, 0, st>>>(x, stride, vec, n, dim, q, e, masks);
+    else pack_kernel<kTypeBF16><<<grid, 256, 0, st>>>(x, stride, vec, n, dim, q, e, masks);
+    return check_launch("pack8");
+}
+
+int neus2_unpack8(int32_t dtype, const int8_t* q, const uint8_t* e, int64_t n, int32_t dim, void* x, int64_t x_stride, void* stream) {
+    NEUS2_TRY(check_pack(dtype, n, dim, x_stride));
+    NEUS2_TRY(check_ptr(q, "q", n > 0));
+    NEUS2_TRY(check_ptr(e, "e", n > 0));
+    NEUS2_TRY(check_ptr(x, "x", n > 0));
+    if (n == 0) return NEUS2_OK;
+    hipStream_t st = (hipStream_t)stream;
+    const int64_t stride = x_stride ? x_stride : dim, blocks = (n * ((dim + 31) / 32 * 4) + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 8 * compute_units() ? blocks : 8 * compute_units());
+    const int vec = rows_aligned(dtype, stride);
+    if (dtype == kTypeF32) unpack_kernel<kTypeF32><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
+    else if (dtype == kTypeF16) unpack_kernel<kTypeF16><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
+    else unpack_kernel<kTypeBF16><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
+    return check_launch("unpack8");
+}
+
+}  // extern "C"
