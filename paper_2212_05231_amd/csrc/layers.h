@@ -47,15 +47,27 @@ struct RowTile {
     int lo, hi;      // its rows
     int part, parts; // which part of the group's rows this is
     int index;       // tiles before this group's first one
+    int shared;      // SHARED: those of groups of more than one tile among them
 };
+
+// inclusive sum over the lanes of a wave
+__device__ __forceinline__ int wave_sums(int v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(v, d);
+        if (lane >= d) v += up;
+    }
+    return v;
+}
 
 // Tile number `tile` when every group's rows are cut into tiles of `rows` rows, at least `least` (0 or 1) tiles a group.  All
 // lanes of the wave take part: 64 groups at a time, one scan over the lanes, so up to 64 groups cost one load's latency.
+template <bool SHARED = false>
 __device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int least, int tile, int lane) {
     RowTile t;
-    t.group = -1; t.lo = t.hi = t.part = t.parts = t.index = 0;
+    t.group = -1; t.lo = t.hi = t.part = t.parts = t.index = t.shared = 0;
     const int count = g.offsets && !g.whole ? g.groups : 1;
-    int before = 0;
+    int before = 0, shared_before = 0;
     for (int base = 0; base < count; base += 64) {
         const int e = base + lane;
         int lo = 0, hi = 0, tiles = 0;
@@ -63,12 +75,8 @@ __device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int leas
             group_rows(g, e, lo, hi);
             tiles = max((hi - lo + rows - 1) / rows, least);
         }
-        int sum = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(sum, d);
-            if (lane >= d) sum += up;
-        }
+        const int sum = wave_sums(tiles, lane), mine = tiles > 1 ? tiles : 0;
+        const int shared = SHARED ? wave_sums(mine, lane) : 0;
         const uint64_t past = __ballot(before + sum > tile);
         if (past) {
             const int at = __builtin_ctzll(past);
@@ -77,14 +85,43 @@ __device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int leas
             hi = __builtin_amdgcn_readlane(hi, at);
             t.parts = __builtin_amdgcn_readlane(tiles, at);
             t.index = before + __builtin_amdgcn_readlane(sum, at) - t.parts;
+            if (SHARED) t.shared = shared_before + __builtin_amdgcn_readlane(shared - mine, at);
             t.part = tile - t.index;
             t.lo = min(lo + t.part * rows, hi);
             t.hi = min(t.lo + rows, hi);
             return t;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
+        if (SHARED) shared_before += __builtin_amdgcn_readlane(shared, 63);
     }
     return t;
+}
+
+// How many tiles there are in all (locate's `rows` and `least`).
+__device__ __forceinline__ int count_tiles(const RowGroups& g, int rows, int least, int lane) {
+    const int count = g.offsets && !g.whole ? g.groups : 1;
+    int total = 0;
+    for (int base = 0; base < count; base += 64) {
+        const int e = base + lane;
+        int lo = 0, hi = 0;
+        if (e < count) {
+            group_rows(g, e, lo, hi);
+            total += max((hi - lo + rows - 1) / rows, least);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    return __builtin_amdgcn_readfirstlane(total);
+}
+
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own.  Of `total` pieces of work in an order in which neighbours
+// read the same memory, every XCD takes a run of consecutive ones.  -1: none for this workgroup (the grid is as large as the pieces
+// may be many, rounded up to a multiple of eight).
+constexpr int kXcds = 8;
+__device__ __forceinline__ int piece_of_block(int total) {
+    const int each = (total + kXcds - 1) / kXcds, local = (int)(blockIdx.x / kXcds);
+    const int piece = (int)(blockIdx.x % kXcds) * each + local;
+    return local < each && piece < total ? piece : -1;
 }
 
 // The segment a row lies in (the last one that begins at or before it), wave-uniform row; S segments.
@@ -214,10 +251,16 @@ struct Packed {
 
 // ---- tiles -----------------------------------------------------------------------------------------------------------------
 // LINES lines of DEPTH steps of the contraction.  ALONG: the contraction runs along the memory rows (x and W in W x).  Planes of
-// [line][DEPTH], a lane reads its eight steps as one 16-byte piece; piece p of a line lies at p ^ swizzle(line), so that eight
-// consecutive lines of one piece cover every bank once.  Otherwise (ACROSS) every memory row is one step of the contraction;
+// [line][DEPTH], a lane reads its eight steps as one 16-byte piece; piece p of a line lies at p ^ swizzle(line), so that sixteen
+// consecutive lines of one piece cover all 64 banks once.  Otherwise (ACROSS) every memory row is one step of the contraction;
 // planes of [DEPTH][line], read back transposed by ds_read_b64_tr_b16 (sixteen lanes read four rows of sixteen values, lane c
-// gets column c); piece p of row k lies at p ^ 2 (k % 4), so that the four rows fall on different banks.
+// gets column c); piece p of row k lies at p ^ across(k), so that the four rows of sixteen lanes fall on different banks, and so do
+// those of thirty-two lanes.
+template <int LINES>
+__device__ __forceinline__ constexpr int across_swizzle(int k) {
+    return LINES == 64 ? ((k & 2) << 1) | ((k & 1) << 1) : ((k & 1) << 2) | (k & 2) | ((k & 2) << 2);
+}
+
 template <class Factor, bool ALONG, int LINES, int DEPTH, int THREADS>
 struct FactorTile {
     static constexpr int kTerms = Factor::kTerms;
@@ -229,7 +272,8 @@ struct FactorTile {
     static_assert(ALONG ? (DEPTH == 32 || DEPTH == 64) : LINES >= 64, "the swizzle needs whole sets of banks");
     typename Factor::Raw raw[kPer];
 
-    __device__ static __forceinline__ int swizzle(int line) { return DEPTH == 64 ? line & 7 : (line >> 1) & 3; }
+    __device__ static __forceinline__ int across(int k) { return across_swizzle<LINES>(k); }
+    __device__ static __forceinline__ int swizzle(int line) { return DEPTH == 64 ? (line >> 1) & 7 : (line >> 2) & 3; }
 
     // lines0, step0: where the tile begins; lines, steps: how many there are in all (the rest is zero)
     __device__ __forceinline__ void load(const typename Factor::Pointer& f, int64_t line0, int lines, int64_t step0, int steps, int tid) {
@@ -250,7 +294,7 @@ struct FactorTile {
             const int r = unit / kPieces, piece = unit % kPieces;
             u32x4 t[kTerms];
             Factor::terms(raw[k], t);
-            const int at = r * kPieces * 16 + ((piece ^ (ALONG ? swizzle(r) : (r & 3) << 1)) << 4);
+            const int at = r * kPieces * 16 + ((piece ^ (ALONG ? swizzle(r) : across(r))) << 4);
 #pragma unroll
             for (int term = 0; term < kTerms; ++term) *reinterpret_cast<u32x4*>(lds + term * kPlane + at) = t[term];
         }
@@ -264,7 +308,7 @@ struct FactorTile {
             typedef short v4s __attribute__((ext_vector_type(4)));
             const int quad = (lane >> 2) & 3;
             const int piece = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-            const unsigned char* at = lds + term * kPlane + (16 * ks + 8 * (lane >> 5) + quad) * (LINES * 2) + ((piece ^ (quad << 1)) << 4) + (lane & 1) * 8;
+            const unsigned char* at = lds + term * kPlane + (16 * ks + 8 * (lane >> 5) + quad) * (LINES * 2) + ((piece ^ across(quad)) << 4) + (lane & 1) * 8;
             const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at));
             const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at + 4 * (LINES * 2)));
             return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -297,19 +341,227 @@ __device__ __forceinline__ v16f mma_terms(const u32x4 (&a)[TA], const u32x4 (&b)
 }
 
 // ---- conversions to the stored type -------------------------------------------------------------------------------------------
-// four consecutive values of a row; `room`: how many of them lie inside the row; vec: rows begin on multiples of four values
-template <int DT>
-__device__ __forceinline__ void store4(typename TypeOf<DT>::Element* p, const v4f& v, int room, bool vec) {
-    typedef typename TypeOf<DT>::Element E;
-    typedef E E4 __attribute__((ext_vector_type(4)));
-    if (room >= 4 && vec) {
-        *reinterpret_cast<E4*>(p) = __builtin_convertvector(v, E4);        // to the nearest, ties to even
+// 16 bytes of a row; `room`: how many of their values lie inside the row; vec: rows begin on multiples of 16 bytes
+template <class E>
+__device__ __forceinline__ void store_piece(E* p, const u32x4& v, int room, bool vec) {
+    constexpr int kValues = 16 / (int)sizeof(E);
+    typedef E Values __attribute__((ext_vector_type(kValues)));
+    if (room >= kValues && vec) {
+        *reinterpret_cast<u32x4*>(p) = v;
     } else {
+        const Values w = __builtin_bit_cast(Values, v);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            if (s < room) p[s] = (E)v[s];
+        for (int s = 0; s < kValues; ++s)
+            if (s < room) p[s] = w[s];
     }
 }
+
+// zero below zero, NaN stays NaN
+__device__ __forceinline__ float relu1(float z) { return z <= 0.f ? 0.f : z; }
+
+// ---- rows through a matrix ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int slot_of(const int32_t* __restrict__ slots, int n_slots, int segment) {
+    const int s = slots ? slots[segment] : segment;
+    return s >= 0 && s < n_slots ? s : -1;
+}
+
+struct RowsArgs {
+    RowGroups groups;
+    const void* x; int64_t x_stride; int x_vec;            // the data rows: x forward, dy backward
+    const void* w; int64_t w_group; int w_stride, w_vec;   // matrix of group g at w + g * w_group, memory rows of w_stride values
+    int steps;                                             // length of the contraction
+    int cols;                                              // outputs per row
+    void* y; int64_t y_stride; int y_vec;
+    int relu;
+    const uint32_t* masks; int mask_words;                 // NULL, or: outputs whose bit is not set are zero
+    // adapters: y += bank[slot] u for the rows of each segment
+    const int32_t* segments; int n_segments;
+    const int32_t* slots; int n_slots;
+    const float* u; const void* bank; int rank;
+    int col_tiles;
+};
+
+// The number of bf16 terms an adapter's fp32 u and its bank matrix take in y += bank u.
+template <int DT> struct AdapterTerms {
+    static constexpr int kU = DT == kTypeF32 ? 3 : 2;
+    static constexpr int kBank = DT == kTypeF32 ? 3 : DT == kTypeF16 ? 2 : 1;
+};
+
+// eight values of a row (k .. k + 7 of `rank`) as floats, zero where the row counts for nothing
+__device__ __forceinline__ f32x8 load_u(const float* __restrict__ u, int64_t row, int rank, int k, bool counts) {
+    f32x8 v;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v[s] = 0.f;
+    if (!counts) return v;
+    const float* p = u + row * rank + k;
+    if ((rank & 7) == 0 && k < rank) {
+        const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+        if (k + s < rank) v[s] = p[s];
+    return v;
+}
+
+// eight values bank(col, k .. k + 7): along the memory row forward (bank [col][rank]), down the column backward ([rank][cols])
+template <int DT, bool BACKWARD>
+__device__ __forceinline__ f32x8 load_bank(const typename TypeOf<DT>::Element* __restrict__ bank, int rank, int cols, int col, int k) {
+    f32x8 v;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v[s] = 0.f;
+    if (col >= cols) return v;
+    if (!BACKWARD && (rank & 7) == 0 && k < rank) {
+        typedef typename TypeOf<DT>::Element E;
+        typedef E E4 __attribute__((ext_vector_type(4)));
+        const E* p = bank + (int64_t)col * rank + k;
+        const E4 a = *reinterpret_cast<const E4*>(p), b = *reinterpret_cast<const E4*>(p + 4);
+        return __builtin_convertvector(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), f32x8);
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+        if (k + s < rank) v[s] = (float)(BACKWARD ? bank[(int64_t)(k + s) * cols + col] : bank[(int64_t)col * rank + k + s]);
+    return v;
+}
+
+// What follows the contraction, for one wave's kBC x kBR blocks of 32 outputs (from col0 on) and 32 rows (from t.lo + row0 on).  A
+// lane holds four times four consecutive outputs of one row in each block.  lds: kBC * 1024 values for each wave, of which nobody
+// reads anything any more.
+template <int DT, bool BACKWARD, bool ADAPT, int kBC, int kBR>
+__device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t, int col0, int row0, v16f (&acc)[kBC][kBR],
+                                            unsigned char* lds, int wave, int lane) {
+    typedef typename TypeOf<DT>::Element E;
+    const int j = lane & 31, h = lane >> 5;
+    if (ADAPT) {
+        // y += bank[slot] u, segment after segment: operands straight from memory (a lane's eight values lie together), the rows of
+        // other segments zero.  A tile inside one segment takes rank / 16 more k-steps.
+        constexpr int kU = AdapterTerms<DT>::kU, kBank = AdapterTerms<DT>::kBank;
+        int s = segment_of(a.segments, a.n_segments, t.lo, lane);
+        for (; s < a.n_segments; ++s) {
+            const int lo = max(a.segments[s], t.lo), hi = min(a.segments[s + 1], t.hi);
+            if (lo >= t.hi) break;
+            const int slot = hi > lo ? slot_of(a.slots, a.n_slots, s) : -1;
+            if (slot < 0) continue;
+            const E* bank = reinterpret_cast<const E*>(a.bank) + (int64_t)slot * a.rank * a.cols;
+            for (int k0 = 0; k0 < a.rank; k0 += 16) {
+                u32x4 u[kBR][kU];
+#pragma unroll
+                for (int r = 0; r < kBR; ++r) {
+                    const int row = t.lo + row0 + 32 * r + j;
+                    split8<kU>(load_u(a.u, row, a.rank, k0 + 8 * h, row >= lo && row < hi), u[r]);
+                }
+#pragma unroll
+                for (int c = 0; c < kBC; ++c) {
+                    u32x4 b[kBank];
+                    split8<kBank>(load_bank<DT, BACKWARD>(bank, a.rank, a.cols, col0 + 32 * c + j, k0 + 8 * h), b);
+#pragma unroll
+                    for (int r = 0; r < kBR; ++r) {
+                        const int first = t.lo + row0 + 32 * r;
+                        if (first >= hi || first + 32 <= lo) continue;
+                        const v16f sum = mma_terms<false>(b, u[r], acc[c][r]);
+                        // an infinite or NaN value of this adapter is nothing to the other segments' rows (0 * inf)
+                        const bool in = (first >= lo && first + 32 <= hi) || (first + j >= lo && first + j < hi);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[c][r][e] = in ? sum[e] : acc[c][r][e];
+                    }
+                }
+            }
+        }
+    }
+    // A block of 32 rows goes through this wave's part of LDS, so that the stores cover whole lines: a lane's four outputs of a row lie
+    // 8 or 16 bytes wide in memory, and stored as they are they took a third of the time of a wide layer (16384 x 2048 x 4096: 318 us
+    // against 217 without any stores).  Pieces of 16 bytes (and the halves of 8 in them) are spread over the banks by row.
+    typedef E E4 __attribute__((ext_vector_type(4)));
+    constexpr int kRowBytes = kBC * 32 * (int)sizeof(E), kPieces = kRowBytes / 16, kRowsAtOnce = 64 / kPieces;
+    constexpr int kValues = 16 / (int)sizeof(E);                         // in a piece
+    static_assert(kRowBytes == 128 || kRowBytes == 256, "the spreading needs rows of half a set of banks or a whole one");
+    unsigned char* mine = lds + wave * 32 * kRowBytes;
+    auto spread = [&](int row) { return kPieces == 16 ? row & 15 : (row >> 1) & 7; };
+#pragma unroll
+    for (int r = 0; r < kBR; ++r) {
+        const int first = t.lo + row0 + 32 * r, row = min(first + j, t.hi - 1);
+#pragma unroll
+        for (int c = 0; c < kBC; ++c) {
+            const int block = min(col0 + 32 * c, a.cols - 1) & ~31;
+            const uint32_t mask = a.masks ? a.masks[(int64_t)row * a.mask_words + (block >> 5)] : 0xffffffffu;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                v4f v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float z = acc[c][r][4 * g + e];
+                    v[e] = (mask >> (8 * g + 4 * h + e)) & 1u ? (a.relu ? relu1(z) : z) : 0.f;
+                }
+                const E4 rounded = __builtin_convertvector(v, E4);       // to the nearest, ties to even
+                const int quad = 8 * c + 2 * g + h;                      // of four outputs
+                if constexpr (sizeof(E) == 4) *reinterpret_cast<E4*>(mine + j * kRowBytes + ((quad ^ spread(j)) << 4)) = rounded;
+                else *reinterpret_cast<E4*>(mine + j * kRowBytes + (((quad >> 1) ^ spread(j)) << 4) + (((quad ^ (j >> 4)) & 1) << 3)) = rounded;
+            }
+        }
+        wave_lds_fence();
+#pragma unroll
+        for (int q = 0; q < 32 / kRowsAtOnce; ++q) {
+            const int at = kRowsAtOnce * q + lane / kPieces, piece = lane % kPieces, col = col0 + piece * kValues;
+            u32x4 v = *reinterpret_cast<const u32x4*>(mine + at * kRowBytes + ((piece ^ spread(at)) << 4));
+            if (sizeof(E) == 2 && q >= 16 / kRowsAtOnce) v = __builtin_shufflevector(v, v, 2, 3, 0, 1);
+            if (first + at < t.hi) store_piece<E>(reinterpret_cast<E*>(a.y) + (int64_t)(first + at) * a.y_stride + col, v, a.cols - col, a.y_vec);
+        }
+        wave_lds_fence();
+    }
+}
+
+// ---- sums over rows -----------------------------------------------------------------------------------------------------------
+struct SumArgs {
+    RowGroups groups;
+    int chunk;                       // rows a workgroup sums over
+    const void* left; int64_t left_stride; int left_vec;
+    const void* right; const uint8_t* right_e; int64_t right_stride; int right_vec;
+    int outer, inner;
+    float* out; int accumulate;
+    float* partial;                  // [partials][outer][inner]: sums of chunks, of all of them (by_slot) or of those that share a group
+    int partials;
+    int by_slot;
+    int outer_tiles, inner_tiles;
+};
+
+// Where a chunk's sums belong, and whether they are added to what is there; NULL: nowhere.
+__device__ __forceinline__ float* sums_place(const SumArgs& a, const RowTile& t, bool& add) {
+    const int64_t size = (int64_t)a.outer * a.inner;
+    add = false;
+    if (!a.by_slot && t.parts == 1) {
+        add = a.accumulate != 0;
+        return a.out + t.group * size;
+    }
+    const int index = (a.by_slot ? t.index : t.shared) + t.part;
+    return t.hi > t.lo && index < a.partials ? a.partial + index * size : nullptr;     // decreasing offsets may count too many
+}
+
+template <int kBO, int kBI>
+__device__ __forceinline__ void store_sums(const SumArgs& a, const RowTile& t, int outer0, int inner0, v16f (&acc)[kBO][kBI], int lane) {
+    bool add;
+    float* out = sums_place(a, t, add);
+    if (!out) return;
+    const int j = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < kBI; ++i) {
+        const int col = inner0 + 32 * i + j;
+        if (col >= a.inner) continue;
+#pragma unroll
+        for (int o = 0; o < kBO; ++o)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = outer0 + 32 * o + neuron_of(r, h);
+                if (row >= a.outer) continue;
+                float* p = out + (int64_t)row * a.inner + col;
+                const float v = acc[o][i][r];
+                *p = add ? *p + v : v;
+            }
+    }
+}
+
+constexpr int kWideOuter = 256, kWideInner = 256;       // their tiles
+void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st);
+int launch_wide_rows(int dtype, bool backward, const RowsArgs& a, hipStream_t st);      // 16-bit types, whole lines of the contraction
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------
 // out[g] (+)= sum over the rows of group g of left_i right_i^T, out [groups][outer][inner] fp32.  left is dy (of the layer's type) or
@@ -325,25 +577,21 @@ struct MatrixGradient {
     float* partial;
     bool by_slot; const int32_t* slots; int n_slots;
 };
-int64_t matrix_gradient_bytes(int groups, int64_t n, int outer, int inner, bool by_slot);
+int64_t matrix_gradient_bytes(const MatrixGradient& m);
 int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st);
-
-__device__ __forceinline__ int slot_of(const int32_t* __restrict__ slots, int n_slots, int segment) {
-    const int s = slots ? slots[segment] : segment;
-    return s >= 0 && s < n_slots ? s : -1;
-}
 
 inline int element_bytes(int dtype) { return dtype == kTypeF32 ? 4 : 2; }
 
 // rows of `stride` values begin on 16-byte boundaries
 inline int rows_aligned(int dtype, int64_t stride) { return (stride * element_bytes(dtype)) % 16 == 0; }
 
+inline int64_t row_tiles(const RowGroups& g, int rows) {
+    return ((int64_t)g.n + rows - 1) / rows + (g.offsets && !g.whole ? g.groups : 0);
+}
+
 inline int check_grid(int64_t blocks) {
     if (blocks > 0x7fffffff) return fail(NEUS2_ERR_SHAPE, "%lld workgroups: too many rows for so many outputs", (long long)blocks);
     return NEUS2_OK;
 }
-
-// zero below zero, NaN stays NaN
-__device__ __forceinline__ float relu1(float z) { return z <= 0.f ? 0.f : z; }
 
 }  // namespace neus2

@@ -5,65 +5,6 @@
 namespace neus2 {
 namespace {
 
-struct RowsArgs {
-    RowGroups groups;
-    const void* x; int64_t x_stride; int x_vec;            // the data rows: x forward, dy backward
-    const void* w; int64_t w_group; int w_stride, w_vec;   // matrix of group g at w + g * w_group, memory rows of w_stride values
-    int steps;                                             // length of the contraction
-    int cols;                                              // outputs per row
-    void* y; int64_t y_stride; int y_vec;
-    int relu;
-    const uint32_t* masks; int mask_words;                 // NULL, or: outputs whose bit is not set are zero
-    // adapters: y += bank[slot] u for the rows of each segment
-    const int32_t* segments; int n_segments;
-    const int32_t* slots; int n_slots;
-    const float* u; const void* bank; int rank;
-    int col_tiles;
-};
-
-// The number of bf16 terms an adapter's fp32 u and its bank matrix take in y += bank u.
-template <int DT> struct AdapterTerms {
-    static constexpr int kU = DT == kTypeF32 ? 3 : 2;
-    static constexpr int kBank = DT == kTypeF32 ? 3 : DT == kTypeF16 ? 2 : 1;
-};
-
-// eight values of a row (k .. k + 7 of `rank`) as floats, zero where the row counts for nothing
-__device__ __forceinline__ f32x8 load_u(const float* __restrict__ u, int64_t row, int rank, int k, bool counts) {
-    f32x8 v;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) v[s] = 0.f;
-    if (!counts) return v;
-    const float* p = u + row * rank + k;
-    if ((rank & 7) == 0 && k < rank) {
-        const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-        if (k + s < rank) v[s] = p[s];
-    return v;
-}
-
-// eight values bank(col, k .. k + 7): along the memory row forward (bank [col][rank]), down the column backward ([rank][cols])
-template <int DT, bool BACKWARD>
-__device__ __forceinline__ f32x8 load_bank(const typename TypeOf<DT>::Element* __restrict__ bank, int rank, int cols, int col, int k) {
-    f32x8 v;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) v[s] = 0.f;
-    if (col >= cols) return v;
-    if (!BACKWARD && (rank & 7) == 0 && k < rank) {
-        typedef typename TypeOf<DT>::Element E;
-        typedef E E4 __attribute__((ext_vector_type(4)));
-        const E* p = bank + (int64_t)col * rank + k;
-        const E4 a = *reinterpret_cast<const E4*>(p), b = *reinterpret_cast<const E4*>(p + 4);
-        return __builtin_convertvector(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), f32x8);
-    }
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-        if (k + s < rank) v[s] = (float)(BACKWARD ? bank[(int64_t)(k + s) * cols + col] : bank[(int64_t)col * rank + k + s]);
-    return v;
-}
-
 // ---- the product engine ----------------------------------------------------------------------------------------------------
 // One workgroup owns ROWS data rows of one group and COLS outputs; both factors of DEPTH steps of the contraction lie in LDS,
 // fetched into registers while the products of the steps before run.  The matrix's tile is the instruction's first operand, so a
@@ -79,7 +20,8 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
     typedef FactorTile<Factor, true, ROWS, DEPTH, kThreads> DataTile;
     typedef FactorTile<Factor, !BACKWARD, COLS, DEPTH, kThreads> MatrixTile;
     constexpr int kBuf = DataTile::kBytes + MatrixTile::kBytes;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[BUFS * kBuf];
+    constexpr int kStores = WR * WC * 32 * kBC * 32 * (int)sizeof(E);
+    __shared__ __attribute__((aligned(16))) unsigned char lds[BUFS * kBuf > kStores ? BUFS * kBuf : kStores];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
@@ -141,58 +83,7 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
         __syncthreads();
     }
 
-    const int j = lane & 31, h = lane >> 5;
-    if (ADAPT) {
-        // y += bank[slot] u, segment after segment: operands straight from memory (a lane's eight values lie together), the rows of
-        // other segments zero.  A tile inside one segment takes rank / 16 more k-steps.
-        constexpr int kU = AdapterTerms<DT>::kU, kBank = AdapterTerms<DT>::kBank;
-        int s = segment_of(a.segments, a.n_segments, t.lo, lane);
-        for (; s < a.n_segments; ++s) {
-            const int lo = max(a.segments[s], t.lo), hi = min(a.segments[s + 1], t.hi);
-            if (lo >= t.hi) break;
-            const int slot = hi > lo ? slot_of(a.slots, a.n_slots, s) : -1;
-            if (slot < 0) continue;
-            const E* bank = reinterpret_cast<const E*>(a.bank) + (int64_t)slot * a.rank * a.cols;
-            for (int k0 = 0; k0 < a.rank; k0 += 16) {
-                u32x4 b[kBC][kBank];
-#pragma unroll
-                for (int c = 0; c < kBC; ++c)
-                    split8<kBank>(load_bank<DT, BACKWARD>(bank, a.rank, a.cols, col0 + 32 * (wc * kBC + c) + j, k0 + 8 * h), b[c]);
-#pragma unroll
-                for (int r = 0; r < kBR; ++r) {
-                    const int first = t.lo + 32 * (wr * kBR + r), row = first + j;
-                    if (first >= hi || first + 32 <= lo) continue;
-                    u32x4 u[kU];
-                    split8<kU>(load_u(a.u, row, a.rank, k0 + 8 * h, row >= lo && row < hi), u);
-#pragma unroll
-                    for (int c = 0; c < kBC; ++c) acc[c][r] = mma_terms<false>(b[c], u, acc[c][r]);
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < kBR; ++r) {
-        const int row = t.lo + 32 * (wr * kBR + r) + j;
-        if (row >= t.hi) continue;
-        E* out = reinterpret_cast<E*>(a.y) + (int64_t)row * a.y_stride;
-#pragma unroll
-        for (int c = 0; c < kBC; ++c) {
-            const int block = col0 + 32 * (wc * kBC + c);
-            if (block >= a.cols) continue;
-            const uint32_t mask = a.masks ? a.masks[(int64_t)row * a.mask_words + (block >> 5)] : 0xffffffffu;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = block + 8 * g + 4 * h;
-                v4f v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float z = acc[c][r][4 * g + e];
-                    v[e] = (mask >> (8 * g + 4 * h + e)) & 1u ? (a.relu ? relu1(z) : z) : 0.f;
-                }
-                store4<DT>(out + col, v, a.cols - col, a.y_vec);
-            }
-        }
-    }
+    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR>(a, t, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------
@@ -420,10 +311,6 @@ __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ 
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------------------
-int64_t row_tiles(const RowGroups& g, int rows) {
-    return ((int64_t)g.n + rows - 1) / rows + (g.offsets && !g.whole ? g.groups : 0);
-}
-
 template <int DT, bool BACKWARD, bool ADAPT>
 int launch_rows(RowsArgs a, hipStream_t st) {
     constexpr int kDepth = DT == kTypeF32 ? 32 : 64, kBufs = DT == kTypeF32 ? 1 : 2;
@@ -438,8 +325,15 @@ int launch_rows(RowsArgs a, hipStream_t st) {
     return check_launch(BACKWARD ? "layer backward" : "layer forward");
 }
 
+// The wide form wants 16-byte rows, a contraction of whole lines, and enough 256 x 256 tiles to be worth its size.
+bool wide_rows_fit(int dtype, const RowsArgs& a) {
+    return dtype != kTypeF32 && a.x_vec && a.w_vec && a.steps % 64 == 0 && a.cols >= 256 && a.x_stride < (1 << 21) &&
+           a.groups.n >= 128 * (a.groups.offsets && !a.groups.whole ? (int64_t)a.groups.groups : 2);
+}
+
 template <bool BACKWARD>
 int launch_rows(int dtype, const RowsArgs& a, hipStream_t st) {
+    if (wide_rows_fit(dtype, a)) return launch_wide_rows(dtype, BACKWARD, a, st);
     if (a.rank > 0) {
         if (dtype == kTypeF32) return launch_rows<kTypeF32, BACKWARD, true>(a, st);
         if (dtype == kTypeF16) return launch_rows<kTypeF16, BACKWARD, true>(a, st);
@@ -560,14 +454,18 @@ int neus2_grouped_fwd(const neus2_layer* l, const void* x, const void* W, const 
     a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
     a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
     a.steps = l->in_dim; a.cols = l->out_dim;
-    a.y = y; a.y_stride = y_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+    a.y = y; a.y_stride = y_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
     a.relu = l->relu;
     return launch_rows<false>(l->dtype, a, st);
 }
 
 int64_t neus2_grouped_workspace_bytes(const neus2_layer* l, int64_t n) {
     if (check_layer(l, false) != NEUS2_OK || check_count(n, "n") != NEUS2_OK) return -1;
-    return matrix_gradient_bytes(l->groups, n, l->out_dim, l->in_dim, false);
+    MatrixGradient m = {};
+    m.groups = make_groups(nullptr, l->groups, n, false);
+    m.dtype = l->dtype;
+    m.outer = l->out_dim; m.inner = l->in_dim;
+    return matrix_gradient_bytes(m);
 }
 
 int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, const uint8_t* xe, const uint32_t* masks, const void* W,
@@ -584,7 +482,7 @@ int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
     NEUS2_TRY(check_ptr(dx, "dx", false));
     NEUS2_TRY(check_ptr(dW, "dW", false));
     NEUS2_TRY(check_ptr(workspace, "workspace", false));
-    const int64_t need = dW ? matrix_gradient_bytes(l->groups, n, l->out_dim, l->in_dim, false) : 0;
+    const int64_t need = dW ? neus2_grouped_workspace_bytes(l, n) : 0;
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(NEUS2_ERR_SHAPE, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)need);
     hipStream_t st = (hipStream_t)stream;
@@ -594,7 +492,7 @@ int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
         a.x = dy; a.x_stride = y_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
         a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
         a.steps = l->out_dim; a.cols = l->in_dim;
-        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
         a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
         NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
     }
@@ -644,7 +542,7 @@ int neus2_adapter_fwd(const neus2_layer* l, const void* x, const void* W, const 
     a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
     a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
     a.steps = l->in_dim; a.cols = l->out_dim;
-    a.y = y; a.y_stride = y_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+    a.y = y; a.y_stride = y_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
     a.relu = l->relu;
     a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
     a.u = u; a.bank = B; a.rank = l->rank;
@@ -654,8 +552,14 @@ int neus2_adapter_fwd(const neus2_layer* l, const void* x, const void* W, const 
 int64_t neus2_adapter_workspace_bytes(const neus2_layer* l, int64_t n) {
     if (check_layer(l, true) != NEUS2_OK || check_count(n, "n") != NEUS2_OK) return -1;
     const int64_t v = (n * l->rank * 4 + 15) / 16 * 16;
-    const int64_t da = matrix_gradient_bytes(l->groups, n, l->rank, l->in_dim, true);
-    const int64_t db = matrix_gradient_bytes(l->groups, n, l->out_dim, l->rank, true);
+    MatrixGradient m = {};
+    m.groups = make_groups(nullptr, l->groups, n, false);
+    m.dtype = l->dtype;
+    m.by_slot = true;
+    m.outer = l->rank; m.inner = l->in_dim; m.left = m.right = (const float*)16;      // narrow sums, of fp32 factors
+    const int64_t da = matrix_gradient_bytes(m);
+    m.outer = l->out_dim; m.inner = l->rank;
+    const int64_t db = matrix_gradient_bytes(m);
     return v + (da > db ? da : db);
 }
 
@@ -693,7 +597,7 @@ int neus2_adapter_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
         a.x = dy; a.x_stride = y_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
         a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
         a.steps = l->out_dim; a.cols = l->in_dim;
-        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = a.y_stride % 4 == 0;
+        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
         a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
         a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
         a.u = v; a.bank = A; a.rank = l->rank;

@@ -9,18 +9,6 @@
 namespace neus2 {
 namespace {
 
-struct SumArgs {
-    RowGroups groups;
-    int chunk;                       // rows a workgroup sums over
-    const void* left; int64_t left_stride; int left_vec;
-    const void* right; const uint8_t* right_e; int64_t right_stride; int right_vec;
-    int outer, inner;
-    float* out; int accumulate;
-    float* partial;                  // [chunks][outer][inner]
-    int always_partial;
-    int outer_tiles, inner_tiles;
-};
-
 template <class Factor>
 __device__ __forceinline__ typename Factor::Pointer make_pointer(const void* p, const uint8_t* e, int64_t stride, int vec) {
     typename Factor::Pointer f;
@@ -45,7 +33,7 @@ __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
     const int tiles = a.outer_tiles * a.inner_tiles;
     const int tile = (int)(blockIdx.x % tiles);
     const int outer0 = tile / a.inner_tiles * OUTER, inner0 = tile % a.inner_tiles * INNER;
-    const RowTile t = locate(a.groups, a.chunk, 1, (int)(blockIdx.x / tiles), lane);
+    const RowTile t = locate<true>(a.groups, a.chunk, 1, (int)(blockIdx.x / tiles), lane);
     if (t.group < 0) return;
 
     const typename Left::Pointer left = make_pointer<Left>(a.left, nullptr, a.left_stride, a.left_vec);
@@ -98,108 +86,125 @@ __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
         __syncthreads();
     }
 
-    const bool direct = !a.always_partial && t.parts == 1;
-    if (!direct && rows == 0) return;
-    const int64_t size = (int64_t)a.outer * a.inner;
-    float* out = direct ? a.out + t.group * size : a.partial + (int64_t)(t.index + t.part) * size;
-    const bool add = direct && a.accumulate;
-    const int j = lane & 31, h = lane >> 5;
-#pragma unroll
-    for (int i = 0; i < kBI; ++i) {
-        const int col = inner0 + 32 * (wi * kBI + i) + j;
-        if (col >= a.inner) continue;
-#pragma unroll
-        for (int o = 0; o < kBO; ++o)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = outer0 + 32 * (wo * kBO + o) + neuron_of(r, h);
-                if (row >= a.outer) continue;
-                float* p = out + (int64_t)row * a.inner + col;
-                const float v = acc[o][i][r];
-                *p = add ? *p + v : v;
-            }
-    }
+    store_sums<kBO, kBI>(a, t, outer0 + 32 * wo * kBO, inner0 + 32 * wi * kBI, acc, lane);
 }
 
-// Adds the chunks' sums in the order of their rows.  One workgroup for 1024 elements of one matrix.
+// Adds the chunks' sums.  A workgroup has 64 elements of one matrix; each of its four waves adds every fourth chunk in the order of
+// the rows, then the four sums are added, so the order is always the same.
 struct JoinArgs {
     RowGroups groups;
     int chunk;
     int64_t size;                    // elements of a matrix
     int blocks;                      // workgroups a matrix
-    const float* partial; int chunks;
+    const float* partial; int partials;
     float* out; int accumulate;
     int by_slot; const int32_t* slots; int n_slots;
 };
 
 __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs a) {
-    const int lane = threadIdx.x & 63;
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int matrix = (int)(blockIdx.x / a.blocks);
-    const int64_t first = (int64_t)(blockIdx.x % a.blocks) * 1024 + threadIdx.x;
     const int groups = a.groups.offsets ? a.groups.groups : 1;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    auto add_parts = [&](int index, int parts) {
-        for (int p = 0; p < parts && index + p < a.chunks; ++p) {          // decreasing offsets may count more than there are
-            const float* src = a.partial + (int64_t)(index + p) * a.size + first;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (first + 256 * q < a.size) sum[q] += src[256 * q];
-        }
-    };
+    int at0 = 0, parts0 = 0;                                                     // a group's parts, if there is only one group
     bool mine = a.by_slot != 0;
-    int before = 0;
-    for (int base = 0; base < groups; base += 64) {
-        const int e = base + lane;
-        int lo = 0, hi = 0, tiles = 0;
-        if (e < groups) {
-            group_rows(a.groups, e, lo, hi);
-            tiles = max((hi - lo + a.chunk - 1) / a.chunk, 1);
-        }
-        int end = tiles;
+    for (int64_t first = (int64_t)(blockIdx.x % a.blocks) * 64; first < a.size; first += (int64_t)a.blocks * 64) {
+        const int64_t at = first + lane;
+        const bool in = at < a.size;
+        float sum = 0.f;
+        int turn = 0;                                                            // chunks so far, modulo the waves
+        auto add_parts = [&](int index, int parts) {
+            const int end = min(index + parts, a.partials);                      // decreasing offsets may count too many
+            int p = index + ((wave - turn) & 3);
+            turn = (turn + parts) & 3;
+            if (!in) return;
+            const float* src = a.partial + at;
+            for (; p + 12 < end; p += 16) {
+                float v[4];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(end, d);
-            if (lane >= d) end += up;
+                for (int q = 0; q < 4; ++q) v[q] = src[(int64_t)(p + 4 * q) * a.size];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum += v[q];
+            }
+            for (; p < end; p += 4) sum += src[(int64_t)p * a.size];
+        };
+        if (parts0 > 0) {
+            add_parts(at0, parts0);
+        } else {
+            int before = 0;
+            for (int base = 0; base < groups; base += 64) {
+                const int e = base + lane;
+                int lo = 0, hi = 0, tiles = 0;
+                if (e < groups) {
+                    group_rows(a.groups, e, lo, hi);
+                    tiles = max((hi - lo + a.chunk - 1) / a.chunk, 1);
+                }
+                if (!a.by_slot && tiles == 1) tiles = 0;                         // stored where it belongs already
+                const int end = wave_sums(tiles, lane);
+                bool match = tiles > 0 && hi > lo;
+                if (a.by_slot) match = match && slot_of(a.slots, a.n_slots, e) == matrix;
+                else match = match && e == matrix;
+                uint64_t set = __ballot(match);
+                while (set) {
+                    const int g = __builtin_ctzll(set);
+                    set &= set - 1;
+                    const int parts = __builtin_amdgcn_readlane(tiles, g), index = before + __builtin_amdgcn_readlane(end, g) - parts;
+                    add_parts(index, parts);
+                    if (!a.by_slot) { at0 = index; parts0 = parts; }
+                    mine = true;
+                }
+                before += __builtin_amdgcn_readlane(end, 63);
+                if (!a.by_slot && matrix < base + 64) break;
+            }
         }
-        bool match = e < groups && hi > lo && e == matrix && tiles > 1;          // one chunk: stored where it belongs already
-        if (a.by_slot) match = e < groups && hi > lo && slot_of(a.slots, a.n_slots, e) == matrix;
-        uint64_t set = __ballot(match);
-        while (set) {
-            const int at = __builtin_ctzll(set);
-            set &= set - 1;
-            const int parts = __builtin_amdgcn_readlane(tiles, at);
-            add_parts(before + __builtin_amdgcn_readlane(end, at) - parts, parts);
-            mine = true;
+        if (!mine) return;                                                       // the same in all four waves
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && in) {
+            float* out = a.out + (int64_t)matrix * a.size + at;
+            const float total = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            *out = a.accumulate ? *out + total : total;
         }
-        before += __builtin_amdgcn_readlane(end, 63);
-        if (!a.by_slot && matrix < base + 64) break;
+        __syncthreads();
     }
-    if (!mine) return;
-    float* out = a.out + (int64_t)matrix * a.size + first;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        if (first + 256 * q < a.size) out[256 * q] = a.accumulate ? out[256 * q] + sum[q] : sum[q];
 }
 
 // ---- how the work is cut --------------------------------------------------------------------------------------------------------
-int tile_of(int dim) { return dim > 64 ? 128 : 64; }
-
-// Rows a workgroup sums over: all of them where the tiles of one matrix alone fill the chip, else as many as give about 512
-// workgroups if one group had all the rows.
-constexpr int kLeastChunk = 256;
-
-int64_t splits_of(int outer, int inner) {
-    const int64_t tiles = (int64_t)((outer + tile_of(outer) - 1) / tile_of(outer)) * ((inner + tile_of(inner) - 1) / tile_of(inner));
-    return tiles >= 256 ? 1 : 512 / tiles;
+// Matrices of at least 256 x 256 in 16-bit types take the wide tiles (layers_wide.hip), if memory rows begin on 16 bytes.
+bool wide_sums_fit(const MatrixGradient& m) {
+    return m.dtype != kTypeF32 && !m.left && !m.right && m.outer >= 256 && m.inner >= 256;
 }
 
-int chunk_rows(int64_t n, int outer, int inner) {
-    const int64_t splits = splits_of(outer, inner);
+int tile_of(int dim) { return dim > 64 ? 128 : 64; }
+
+int64_t tiles_of(int outer, int inner, bool wide) {
+    const int to = wide ? kWideOuter : tile_of(outer), ti = wide ? kWideInner : tile_of(inner);
+    return (int64_t)((outer + to - 1) / to) * ((inner + ti - 1) / ti);
+}
+
+// Rows a workgroup sums over: all of them where the tiles of one matrix alone fill the chip, else so many that one group with all
+// the rows would give about 512 workgroups (256 of the wide ones, of which a compute unit takes one at a time).
+constexpr int kLeastChunk = 256;
+
+int64_t splits_of(int outer, int inner, bool wide) {
+    const int64_t tiles = tiles_of(outer, inner, wide);
+    return tiles >= 256 ? 1 : ((wide ? 256 : 512) + tiles - 1) / tiles;
+}
+
+int chunk_rows(int64_t n, int64_t splits) {
     const int64_t rows = ((n + splits - 1) / splits + 127) / 128 * 128;
     return (int)(rows < kLeastChunk ? kLeastChunk : rows);
 }
 
 int64_t chunk_count(int groups, int64_t n, int chunk) { return (n + chunk - 1) / chunk + groups; }
+
+// Chunks whose sums go to the workspace; never fewer for more rows.  By slot: all of them.  Otherwise only those of groups of more
+// than one: a group of L > chunk rows has fewer than 2 L / chunk, all of them together fewer than 2 n / chunk <= 2 splits.
+int64_t partial_count(int groups, int64_t n, int64_t splits, bool by_slot) {
+    const int64_t least = (n + kLeastChunk - 1) / kLeastChunk, chunks = splits < least ? splits : least;
+    if (by_slot) return chunks + groups;
+    return splits == 1 || n <= kLeastChunk ? 0 : 2 * chunks;
+}
 
 template <class Left, class Right, bool HALF, int OUTER, int INNER>
 void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
@@ -209,37 +214,37 @@ void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
 }
 
 template <class Left, class Right, bool HALF>
-int launch_sums(SumArgs a, hipStream_t st) {
-    const int to = tile_of(a.outer), ti = tile_of(a.inner);
-    a.outer_tiles = (a.outer + to - 1) / to;
-    a.inner_tiles = (a.inner + ti - 1) / ti;
-    const int64_t blocks = chunk_count(a.groups.offsets ? a.groups.groups : 1, a.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles;
-    NEUS2_TRY(check_grid(blocks));
-    if (to == 128 && ti == 128) launch_sums<Left, Right, HALF, 128, 128>(a, (unsigned)blocks, st);
-    else if (to == 128) launch_sums<Left, Right, HALF, 128, 64>(a, (unsigned)blocks, st);
-    else if (ti == 128) launch_sums<Left, Right, HALF, 64, 128>(a, (unsigned)blocks, st);
-    else launch_sums<Left, Right, HALF, 64, 64>(a, (unsigned)blocks, st);
-    return check_launch("matrix gradient");
+void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
+    const bool o = a.outer > 64, i = a.inner > 64;
+    if (o && i) launch_sums<Left, Right, HALF, 128, 128>(a, grid, st);
+    else if (o) launch_sums<Left, Right, HALF, 128, 64>(a, grid, st);
+    else if (i) launch_sums<Left, Right, HALF, 64, 128>(a, grid, st);
+    else launch_sums<Left, Right, HALF, 64, 64>(a, grid, st);
 }
 
 }  // namespace
 
-int64_t matrix_gradient_bytes(int groups, int64_t n, int outer, int inner, bool by_slot) {
-    const int64_t splits = splits_of(outer, inner), least = (n + kLeastChunk - 1) / kLeastChunk;
-    if (!by_slot && (splits == 1 || n <= kLeastChunk)) return 0;
-    return ((splits < least ? splits : least) + groups) * outer * inner * 4;      // at least chunk_count, and never less for more rows
+// (aligned or not: the workspace serves both)
+int64_t matrix_gradient_bytes(const MatrixGradient& m) {
+    const bool wide = wide_sums_fit(m);
+    const int64_t count = partial_count(m.groups.groups, m.groups.n, splits_of(m.outer, m.inner, wide), m.by_slot);
+    return count * m.outer * m.inner * 4;
 }
 
 int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
+    const int count = m.groups.offsets ? m.groups.groups : 1;
+    const bool wide = wide_sums_fit(m);
+    const int64_t splits = splits_of(m.outer, m.inner, wide);
     SumArgs a = {};
     a.groups = m.groups;
-    a.chunk = chunk_rows(m.groups.n, m.outer, m.inner);
+    a.chunk = chunk_rows(m.groups.n, splits);
     a.outer = m.outer;
     a.inner = m.inner;
     a.out = m.out;
     a.accumulate = m.accumulate;
     a.partial = m.partial;
-    a.always_partial = m.by_slot;
+    a.partials = (int)partial_count(count, m.groups.n, splits, m.by_slot);
+    a.by_slot = m.by_slot ? 1 : 0;
     if (m.left) {
         a.left = m.left; a.left_stride = m.outer; a.left_vec = m.outer % 4 == 0;
     } else {
@@ -252,39 +257,49 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     } else {
         a.right = m.x; a.right_stride = m.x_stride; a.right_vec = rows_aligned(m.dtype, m.x_stride);
     }
-    int rc;
     const bool f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
+    const bool aligned = a.left_vec && (m.xq || a.right_vec) && m.dy_stride < (1 << 21) && m.x_stride < (1 << 21);
+    const int to = wide && aligned ? kWideOuter : tile_of(m.outer), ti = wide && aligned ? kWideInner : tile_of(m.inner);
+    a.outer_tiles = (a.outer + to - 1) / to;
+    a.inner_tiles = (a.inner + ti - 1) / ti;
+    const int64_t blocks = (chunk_count(count, m.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles + kXcds - 1) / kXcds * kXcds;
+    NEUS2_TRY(check_grid(blocks));
+    const unsigned grid = (unsigned)blocks;
     if (m.left) {                                                       // v x^T
-        if (f32) rc = m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, st) : launch_sums<Wide<3>, Wide<3>, false>(a, st);
-        else if (m.xq) rc = launch_sums<Wide<2>, Packed<false>, false>(a, st);
-        else rc = f16 ? launch_sums<Wide<2>, HalfPair, false>(a, st) : launch_sums<Wide<2>, Native, false>(a, st);
+        if (f32) m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
+        else if (m.xq) launch_sums<Wide<2>, Packed<false>, false>(a, grid, st);
+        else f16 ? launch_sums<Wide<2>, HalfPair, false>(a, grid, st) : launch_sums<Wide<2>, Native, false>(a, grid, st);
     } else if (m.right) {                                               // dy u^T
-        if (f32) rc = launch_sums<Wide<3>, Wide<3>, false>(a, st);
-        else rc = f16 ? launch_sums<HalfPair, Wide<2>, false>(a, st) : launch_sums<Native, Wide<2>, false>(a, st);
+        if (f32) launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
+        else f16 ? launch_sums<HalfPair, Wide<2>, false>(a, grid, st) : launch_sums<Native, Wide<2>, false>(a, grid, st);
     } else if (f32) {
-        rc = m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, st) : launch_sums<Wide<3>, Wide<3>, false>(a, st);
+        m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
+    } else if (wide && aligned) {
+        launch_wide_sums(m.dtype, m.xq != nullptr, a, grid, st);
     } else if (f16) {
-        rc = m.xq ? launch_sums<Native, Packed<true>, true>(a, st) : launch_sums<Native, Native, true>(a, st);
+        m.xq ? launch_sums<Native, Packed<true>, true>(a, grid, st) : launch_sums<Native, Native, true>(a, grid, st);
     } else {
-        rc = m.xq ? launch_sums<Native, Packed<false>, false>(a, st) : launch_sums<Native, Native, false>(a, st);
+        m.xq ? launch_sums<Native, Packed<false>, false>(a, grid, st) : launch_sums<Native, Native, false>(a, grid, st);
     }
-    if (rc != NEUS2_OK) return rc;
-    if (!m.by_slot && m.groups.n <= a.chunk) return NEUS2_OK;           // every group was one chunk
+    NEUS2_TRY(check_launch("matrix gradient"));
+    if (a.partials == 0) return NEUS2_OK;                               // every group was one chunk
     JoinArgs j = {};
     j.groups = m.groups;
     j.chunk = a.chunk;
     j.size = (int64_t)m.outer * m.inner;
-    j.blocks = (int)((j.size + 1023) / 1024);
+    // most groups of a large matrix are one chunk and have nothing to join: few workgroups find that out
+    const int64_t matrices = m.by_slot ? m.n_slots : count, most = (8192 + matrices - 1) / matrices;
+    j.blocks = (int)((j.size + 63) / 64 < most ? (j.size + 63) / 64 : most);
     j.partial = m.partial;
-    j.chunks = (int)chunk_count(m.groups.offsets ? m.groups.groups : 1, m.groups.n, a.chunk);
+    j.partials = a.partials;
     j.out = m.out;
     j.accumulate = m.accumulate;
-    j.by_slot = m.by_slot ? 1 : 0;
+    j.by_slot = a.by_slot;
     j.slots = m.slots;
     j.n_slots = m.n_slots;
-    const int64_t blocks = (m.by_slot ? m.n_slots : m.groups.offsets ? m.groups.groups : 1) * (int64_t)j.blocks;
-    NEUS2_TRY(check_grid(blocks));
-    join_sums_kernel<<<(unsigned)blocks, 256, 0, st>>>(j);
+    const int64_t joins = matrices * j.blocks;
+    NEUS2_TRY(check_grid(joins));
+    join_sums_kernel<<<(unsigned)joins, 256, 0, st>>>(j);
     return check_launch("matrix gradient sums");
 }
 

@@ -1,0 +1,248 @@
+// The wide form of the layers' products for 16-bit types: tiles of 256 x 256 whose factors go from memory to LDS without passing
+// through registers.
+#include "layers.h"
+
+namespace neus2 {
+namespace {
+
+constexpr int kLeft = 256, kRight = 256;         // lines of the instruction's first and second operand
+constexpr int kDepth = 64, kThreads = 512, kWaves = 8, kBand = 8;
+constexpr int kLeftBytes = kLeft * kDepth * 2, kRightBytes = kRight * kDepth * 2;
+
+// A lane's place in the loads of one factor's tile: chunk c of 1024 bytes (one instruction of a wave) holds units 64 c .. 64 c + 63 of
+// 16 bytes in LDS order, and the lane fetches from memory what belongs at its place (FactorTile's order, its swizzle included).
+template <bool ALONG, int LINES>
+struct WideTile {
+    static constexpr int kLoads = LINES * kDepth * 2 / 1024 / kWaves;     // a wave takes every eighth chunk
+    uint32_t offset[kLoads];
+    __device__ __forceinline__ void begin(int64_t stride, int wave, int lane) {
+        typedef FactorTile<Native, ALONG, LINES, kDepth, kThreads> Tile;
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int unit = 64 * (wave + kWaves * q) + lane;
+            const int r = unit / Tile::kPieces, piece = (unit % Tile::kPieces) ^ (ALONG ? Tile::swizzle(r) : Tile::across(r));
+            offset[q] = (uint32_t)r * (uint32_t)stride * 2u + 16u * (uint32_t)piece;
+        }
+    }
+    // from: where the tile begins; bytes: how far memory may be read from there on.  What lies beyond comes back as zero, except that
+    // the last 16 bytes with something to read are read whole.
+    __device__ __forceinline__ void load(const uint16_t* from, int64_t bytes, unsigned char* lds, int wave) const {
+        const int room = (int)(bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : (bytes + 15) & ~15);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, room, 0x00020000);
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (wave + kWaves * q) * 1024), 16, (int)offset[q], 0, 0, 0);
+    }
+};
+
+// All loads to LDS of this wave have arrived, its LDS reads and writes are done, and every wave of the workgroup has got here.
+__device__ __forceinline__ void arrive() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
+// The operands of one k-step of a wave: four blocks of 32 lines of the left factor (the instruction's first operand), two of the right.
+struct Operands {
+    u32x4 l[4], r[2];
+    template <class LeftTile, class RightTile>
+    __device__ __forceinline__ void read(const unsigned char* left, const unsigned char* right, int wl, int wr, int ks, int lane) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) l[c] = LeftTile::operand(left, 0, 4 * wl + c, ks, lane);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) r[c] = RightTile::operand(right, 0, 2 * wr + c, ks, lane);
+    }
+    template <bool HALF, int FIRST, int LAST>
+    __device__ __forceinline__ void multiply(v16f (&acc)[4][2]) const {
+#pragma unroll
+        for (int c = FIRST; c < LAST; ++c)
+#pragma unroll
+            for (int d = 0; d < 2; ++d) acc[c][d] = mma32<HALF>(l[c], r[d], acc[c][d]);
+    }
+};
+
+struct Stages {
+    unsigned char *left[2], *right[2];
+};
+
+// The whole contraction: `rounds` pairs of tiles in two pairs of buffers, the loads of one pair in flight while the products of the
+// pair before run.  A k-step's operands are read while the instructions of the step before run, across the pairs too: the workgroup
+// meets in the middle of a pair's last step, so that the matrix pipe still has work when the waves come out of the barrier and wait for
+// their first operands.  The scheduler is kept from moving reads further up, which would take more registers than there are.
+// fetch(left, right, more) issues a pair's loads (zeros if there is no more: an odd number of pairs ends with one of zeros);
+// land(right) is what a factor that does pass through registers still has to do.
+template <bool HALF, class LeftTile, class RightTile, class Fetch, class Land>
+__device__ __forceinline__ void contract(int rounds, const Fetch& fetch, const Land& land, const Stages& s, int wl, int wr, int lane,
+                                         v16f (&acc)[4][2]) {
+    constexpr int kSteps = kDepth / 16;
+    Operands o[2];
+    fetch(s.left[0], s.right[0], rounds > 0);
+    land(s.right[0]);
+    arrive();
+    o[0].read<LeftTile, RightTile>(s.left[0], s.right[0], wl, wr, 0, lane);
+    for (int k = 0; k < rounds; k += 2) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            fetch(s.left[q ^ 1], s.right[q ^ 1], k + q + 1 < rounds);
+#pragma unroll
+            for (int ks = 0; ks < kSteps - 1; ++ks) {
+                o[(ks + 1) & 1].read<LeftTile, RightTile>(s.left[q], s.right[q], wl, wr, ks + 1, lane);
+                o[ks & 1].multiply<HALF, 0, 4>(acc);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            land(s.right[q ^ 1]);
+            o[1].multiply<HALF, 0, 2>(acc);
+            __builtin_amdgcn_sched_barrier(0);
+            arrive();
+            o[0].read<LeftTile, RightTile>(s.left[q ^ 1], s.right[q ^ 1], wl, wr, 0, lane);
+            o[1].multiply<HALF, 2, 4>(acc);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+#define NEUS2_STAGES                                                                                                      \
+    __shared__ __attribute__((aligned(16))) unsigned char left0[kLeftBytes], left1[kLeftBytes];                           \
+    __shared__ __attribute__((aligned(16))) unsigned char right0[kRightBytes], right1[kRightBytes];                       \
+    const Stages stages = {{left0, left1}, {right0, right1}}
+
+template <int DT, bool BACKWARD, bool ADAPT>
+__global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
+    typedef FactorTile<Native, true, kRight, kDepth, kThreads> DataTile;
+    typedef FactorTile<Native, !BACKWARD, kLeft, kDepth, kThreads> MatrixTile;
+    NEUS2_STAGES;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wc = wave >> 2, wr = wave & 3;
+    // bands of eight tiles of rows, in a band the rows fastest: the workgroups at work on an XCD share few rows and few columns
+    const int row_tiles = count_tiles(a.groups, kRight, 0, lane), piece = piece_of_block(row_tiles * a.col_tiles);
+    if (piece < 0) return;
+    const int band = piece / (kBand * a.col_tiles), within = piece % (kBand * a.col_tiles), deep = min(kBand, row_tiles - band * kBand);
+    const int col0 = within / deep * kLeft;
+    const RowTile t = locate(a.groups, kRight, 0, band * kBand + within % deep, lane);
+
+    WideTile<true, kRight> dt;
+    WideTile<!BACKWARD, kLeft> mt;
+    dt.begin(a.x_stride, wave, lane);
+    mt.begin(a.w_stride, wave, lane);
+    const uint16_t* x = reinterpret_cast<const uint16_t*>(a.x) + (int64_t)t.lo * a.x_stride;
+    const uint16_t* w = reinterpret_cast<const uint16_t*>(a.w) + (int64_t)t.group * a.w_group + (int64_t)col0 * (BACKWARD ? 1 : a.w_stride);
+    int64_t x_bytes = ((int64_t)(t.hi - t.lo - 1) * a.x_stride + a.steps) * 2;
+    int64_t w_bytes = BACKWARD ? ((int64_t)a.steps * a.w_stride - col0) * 2 : (int64_t)(a.cols - col0) * a.w_stride * 2;
+    const int64_t w_step = BACKWARD ? (int64_t)kDepth * a.w_stride : kDepth;
+
+    v16f acc[4][2];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
+    auto fetch = [&](unsigned char* matrix, unsigned char* data, bool more) {
+        dt.load(x, more ? x_bytes : 0, data, wave);
+        mt.load(w, more ? w_bytes : 0, matrix, wave);
+        x += kDepth;
+        x_bytes -= kDepth * 2;
+        w += w_step;
+        w_bytes -= w_step * 2;
+    };
+    contract<DT == kTypeF16, MatrixTile, DataTile>(a.steps / kDepth, fetch, [](unsigned char*) {}, stages, wc, wr, lane, acc);
+    finish_rows<DT, BACKWARD, ADAPT, 4, 2>(a, t, col0 + 128 * wc, 64 * wr, acc, wave < 4 ? left0 : left1, wave & 3, lane);
+}
+
+template <int DT, bool BACKWARD>
+void launch(const RowsArgs& a, unsigned grid, hipStream_t st) {
+    if (a.rank > 0) wide_rows_kernel<DT, BACKWARD, true><<<grid, kThreads, 0, st>>>(a);
+    else wide_rows_kernel<DT, BACKWARD, false><<<grid, kThreads, 0, st>>>(a);
+}
+
+// Sums over rows: both factors lie across (a memory row is a step of the contraction), the rows behind the chunk's last are zeros.
+// PACKED: the right factor is in 8 bits.  A thread then fetches 32 of its values (one block of one row, one exponent) and puts them
+// into LDS as 16-bit numbers at the end of the round.
+template <int DT, bool PACKED>
+__global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
+    constexpr bool kHalf = DT == kTypeF16;
+    typedef FactorTile<Native, false, kLeft, kDepth, kThreads> LeftTile;
+    typedef FactorTile<Native, false, kRight, kDepth, kThreads> RightTile;
+    typedef Packed<kHalf> Factor8;
+    NEUS2_STAGES;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wo = wave >> 2, wi = wave & 3;
+    const int tiles = a.outer_tiles * a.inner_tiles;
+    const int piece = piece_of_block(count_tiles(a.groups, a.chunk, 1, lane) * tiles);
+    if (piece < 0) return;
+    const int tile = piece % tiles;
+    const int outer0 = tile / a.inner_tiles * kLeft, inner0 = tile % a.inner_tiles * kRight;
+    const RowTile t = locate<true>(a.groups, a.chunk, 1, piece / tiles, lane);
+
+    v16f acc[4][2];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
+    WideTile<false, kLeft> lt;
+    WideTile<false, kRight> rt;
+    lt.begin(a.left_stride, wave, lane);
+    rt.begin(a.right_stride, wave, lane);
+    int rows = t.hi - t.lo;
+    const int rounds = (rows + kDepth - 1) / kDepth;
+    const uint16_t* left = reinterpret_cast<const uint16_t*>(a.left) + (int64_t)t.lo * a.left_stride + outer0;
+    const uint16_t* right = reinterpret_cast<const uint16_t*>(a.right) + (PACKED ? 0 : (int64_t)t.lo * a.right_stride + inner0);
+    int64_t row8 = t.lo + (tid >> 3);
+    const int col8 = inner0 + 32 * (tid & 7);
+    typename Factor8::Pointer packed;
+    packed.p = reinterpret_cast<const int8_t*>(a.right);
+    packed.e = a.right_e;
+    packed.stride = a.right_stride;
+    typename Factor8::Raw raw[4];
+    auto fetch = [&](unsigned char* l, unsigned char* r, bool more) {
+        lt.load(left, more ? ((int64_t)(rows - 1) * a.left_stride + a.outer - outer0) * 2 : 0, l, wave);
+        if (PACKED) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) raw[q] = Factor8::load(packed, row8, col8 + 8 * q, more && row8 < t.hi ? a.inner - (col8 + 8 * q) : 0);
+            row8 += kDepth;
+        } else {
+            rt.load(right, more ? ((int64_t)(rows - 1) * a.right_stride + a.inner - inner0) * 2 : 0, r, wave);
+            right += (int64_t)kDepth * a.right_stride;
+        }
+        left += (int64_t)kDepth * a.left_stride;
+        rows -= kDepth;
+    };
+    auto land = [&](unsigned char* r) {
+        if (!PACKED) return;
+        const int line = tid >> 3;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            u32x4 v[1];
+            Factor8::terms(raw[q], v);
+            *reinterpret_cast<u32x4*>(r + line * (kRight * 2) + (((4 * (tid & 7) + q) ^ RightTile::across(line)) << 4)) = v[0];
+        }
+    };
+    contract<kHalf, LeftTile, RightTile>(rounds, fetch, land, stages, wo, wi, lane, acc);
+    store_sums<4, 2>(a, t, outer0 + 128 * wo, inner0 + 64 * wi, acc, lane);
+}
+
+}  // namespace
+
+void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st) {
+    if (dtype == kTypeF16) {
+        if (packed) wide_sums_kernel<kTypeF16, true><<<grid, kThreads, 0, st>>>(a);
+        else wide_sums_kernel<kTypeF16, false><<<grid, kThreads, 0, st>>>(a);
+    } else {
+        if (packed) wide_sums_kernel<kTypeBF16, true><<<grid, kThreads, 0, st>>>(a);
+        else wide_sums_kernel<kTypeBF16, false><<<grid, kThreads, 0, st>>>(a);
+    }
+}
+
+int launch_wide_rows(int dtype, bool backward, const RowsArgs& args, hipStream_t st) {
+    RowsArgs a = args;
+    a.col_tiles = (a.cols + kLeft - 1) / kLeft;
+    const int64_t blocks = (row_tiles(a.groups, kRight) * a.col_tiles + kXcds - 1) / kXcds * kXcds;
+    NEUS2_TRY(check_grid(blocks));
+    const unsigned grid = (unsigned)blocks;
+    if (dtype == kTypeF16) backward ? launch<kTypeF16, true>(a, grid, st) : launch<kTypeF16, false>(a, grid, st);
+    else backward ? launch<kTypeBF16, true>(a, grid, st) : launch<kTypeBF16, false>(a, grid, st);
+    return check_launch("wide layer");
+}
+
+}  // namespace neus2
