@@ -83,7 +83,7 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
         __syncthreads();
     }
 
-    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR>(a, t, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane);
+    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR, false>(a, t, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane, [] {});
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------

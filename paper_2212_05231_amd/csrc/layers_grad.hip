@@ -262,7 +262,7 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     const int to = wide && aligned ? kWideOuter : tile_of(m.outer), ti = wide && aligned ? kWideInner : tile_of(m.inner);
     a.outer_tiles = (a.outer + to - 1) / to;
     a.inner_tiles = (a.inner + ti - 1) / ti;
-    const int64_t blocks = (chunk_count(count, m.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles + kXcds - 1) / kXcds * kXcds;
+    const int64_t blocks = chunk_count(count, m.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles;
     NEUS2_TRY(check_grid(blocks));
     const unsigned grid = (unsigned)blocks;
     if (m.left) {                                                       // v x^T
@@ -275,7 +275,7 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     } else if (f32) {
         m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
     } else if (wide && aligned) {
-        launch_wide_sums(m.dtype, m.xq != nullptr, a, grid, st);
+        launch_wide_sums(m.dtype, m.xq != nullptr, a, blocks, st);
     } else if (f16) {
         m.xq ? launch_sums<Native, Packed<true>, true>(a, grid, st) : launch_sums<Native, Native, true>(a, grid, st);
     } else {

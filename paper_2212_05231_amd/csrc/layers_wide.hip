@@ -6,7 +6,7 @@ namespace neus2 {
 namespace {
 
 constexpr int kLeft = 256, kRight = 256;         // lines of the instruction's first and second operand
-constexpr int kDepth = 64, kThreads = 512, kWaves = 8, kBand = 8;
+constexpr int kDepth = 64, kThreads = 512, kWaves = 8, kBand = 4;
 constexpr int kLeftBytes = kLeft * kDepth * 2, kRightBytes = kRight * kDepth * 2;
 
 // A lane's place in the loads of one factor's tile: chunk c of 1024 bytes (one instruction of a wave) holds units 64 c .. 64 c + 63 of
@@ -35,9 +35,15 @@ struct WideTile {
     }
 };
 
-// All loads to LDS of this wave have arrived, its LDS reads and writes are done, and every wave of the workgroup has got here.
-__device__ __forceinline__ void arrive() {
+// All loads to LDS of this wave have arrived.
+__device__ __forceinline__ void loaded() {
+    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// This wave's LDS reads and writes are done, and every wave of the workgroup has got here.
+__device__ __forceinline__ void meet() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
@@ -71,30 +77,31 @@ struct Stages {
 // meets in the middle of a pair's last step, so that the matrix pipe still has work when the waves come out of the barrier and wait for
 // their first operands.  The scheduler is kept from moving reads further up, which would take more registers than there are.
 // fetch(left, right, more) issues a pair's loads (zeros if there is no more: an odd number of pairs ends with one of zeros);
-// land(right) is what a factor that does pass through registers still has to do.
+// land(right) is what a factor that does pass through registers still has to do.  The caller has issued the first pair's loads and waited
+// for them (loaded()); when this returns nobody reads either pair of buffers any more.
 template <bool HALF, class LeftTile, class RightTile, class Fetch, class Land>
 __device__ __forceinline__ void contract(int rounds, const Fetch& fetch, const Land& land, const Stages& s, int wl, int wr, int lane,
                                          v16f (&acc)[4][2]) {
     constexpr int kSteps = kDepth / 16;
     Operands o[2];
-    fetch(s.left[0], s.right[0], rounds > 0);
     land(s.right[0]);
-    arrive();
+    meet();
     o[0].read<LeftTile, RightTile>(s.left[0], s.right[0], wl, wr, 0, lane);
     for (int k = 0; k < rounds; k += 2) {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            fetch(s.left[q ^ 1], s.right[q ^ 1], k + q + 1 < rounds);
 #pragma unroll
             for (int ks = 0; ks < kSteps - 1; ++ks) {
                 o[(ks + 1) & 1].read<LeftTile, RightTile>(s.left[q], s.right[q], wl, wr, ks + 1, lane);
+                if (ks == 0) fetch(s.left[q ^ 1], s.right[q ^ 1], k + q + 1 < rounds);
                 o[ks & 1].multiply<HALF, 0, 4>(acc);
                 __builtin_amdgcn_sched_barrier(0);
             }
             land(s.right[q ^ 1]);
             o[1].multiply<HALF, 0, 2>(acc);
             __builtin_amdgcn_sched_barrier(0);
-            arrive();
+            loaded();
+            meet();
             o[0].read<LeftTile, RightTile>(s.left[q ^ 1], s.right[q ^ 1], wl, wr, 0, lane);
             o[1].multiply<HALF, 2, 4>(acc);
             __builtin_amdgcn_sched_barrier(0);
@@ -115,28 +122,33 @@ __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wc = wave >> 2, wr = wave & 3;
-    // bands of eight tiles of rows, in a band the rows fastest: the workgroups at work on an XCD share few rows and few columns
-    const int row_tiles = count_tiles(a.groups, kRight, 0, lane), piece = piece_of_block(row_tiles * a.col_tiles);
-    if (piece < 0) return;
-    const int band = piece / (kBand * a.col_tiles), within = piece % (kBand * a.col_tiles), deep = min(kBand, row_tiles - band * kBand);
-    const int col0 = within / deep * kLeft;
-    const RowTile t = locate(a.groups, kRight, 0, band * kBand + within % deep, lane);
+    // bands of four tiles of rows, in a band the rows fastest: the workgroups at work on an XCD share few rows and few columns
+    const int row_tiles = count_tiles(a.groups, kRight, 0, lane);
+    Pieces pieces(row_tiles * a.col_tiles);
+    int col0 = 0;
+    RowTile t;
+    auto place = [&](int piece, int& col, RowTile& tile) {
+        const int band = piece / (kBand * a.col_tiles), within = piece % (kBand * a.col_tiles), deep = min(kBand, row_tiles - band * kBand);
+        col = within / deep * kLeft;
+        tile = locate(a.groups, kRight, 0, band * kBand + within % deep, lane);
+    };
+    const int first = pieces.take();
+    if (first < 0) return;
+    place(first, col0, t);
 
     WideTile<true, kRight> dt;
     WideTile<!BACKWARD, kLeft> mt;
     dt.begin(a.x_stride, wave, lane);
     mt.begin(a.w_stride, wave, lane);
-    const uint16_t* x = reinterpret_cast<const uint16_t*>(a.x) + (int64_t)t.lo * a.x_stride;
-    const uint16_t* w = reinterpret_cast<const uint16_t*>(a.w) + (int64_t)t.group * a.w_group + (int64_t)col0 * (BACKWARD ? 1 : a.w_stride);
-    int64_t x_bytes = ((int64_t)(t.hi - t.lo - 1) * a.x_stride + a.steps) * 2;
-    int64_t w_bytes = BACKWARD ? ((int64_t)a.steps * a.w_stride - col0) * 2 : (int64_t)(a.cols - col0) * a.w_stride * 2;
+    const uint16_t *x, *w;
+    int64_t x_bytes, w_bytes;
     const int64_t w_step = BACKWARD ? (int64_t)kDepth * a.w_stride : kDepth;
-
-    v16f acc[4][2];
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
+    auto begin = [&]() {
+        x = reinterpret_cast<const uint16_t*>(a.x) + (int64_t)t.lo * a.x_stride;
+        w = reinterpret_cast<const uint16_t*>(a.w) + (int64_t)t.group * a.w_group + (int64_t)col0 * (BACKWARD ? 1 : a.w_stride);
+        x_bytes = ((int64_t)(t.hi - t.lo - 1) * a.x_stride + a.steps) * 2;
+        w_bytes = BACKWARD ? ((int64_t)a.steps * a.w_stride - col0) * 2 : (int64_t)(a.cols - col0) * a.w_stride * 2;
+    };
     auto fetch = [&](unsigned char* matrix, unsigned char* data, bool more) {
         dt.load(x, more ? x_bytes : 0, data, wave);
         mt.load(w, more ? w_bytes : 0, matrix, wave);
@@ -145,8 +157,28 @@ __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
         w += w_step;
         w_bytes -= w_step * 2;
     };
-    contract<DT == kTypeF16, MatrixTile, DataTile>(a.steps / kDepth, fetch, [](unsigned char*) {}, stages, wc, wr, lane, acc);
-    finish_rows<DT, BACKWARD, ADAPT, 4, 2>(a, t, col0 + 128 * wc, 64 * wr, acc, wave < 4 ? left0 : left1, wave & 3, lane);
+    begin();
+    fetch(left0, right0, true);
+    loaded();
+    // The first loads of the next tile are under way while this one's outputs are stored (not beside an adapter's part, which takes the
+    // registers: a workgroup then has one tile).
+    for (;;) {
+        v16f acc[4][2];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
+        const RowTile now = t;
+        const int now_col = col0, next = ADAPT ? -1 : pieces.take();
+        if (next >= 0) place(next, col0, t);
+        contract<DT == kTypeF16, MatrixTile, DataTile>(a.steps / kDepth, fetch, [](unsigned char*) {}, stages, wc, wr, lane, acc);
+        if (next >= 0) {
+            begin();
+            fetch(left0, right0, true);
+        }
+        finish_rows<DT, BACKWARD, ADAPT, 4, 2, true>(a, now, now_col + 128 * wc, 64 * wr, acc, wave < 4 ? left1 : right1, wave & 3, lane, loaded);
+        if (next < 0) break;
+    }
 }
 
 template <int DT, bool BACKWARD>
@@ -169,40 +201,49 @@ __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wo = wave >> 2, wi = wave & 3;
     const int tiles = a.outer_tiles * a.inner_tiles;
-    const int piece = piece_of_block(count_tiles(a.groups, a.chunk, 1, lane) * tiles);
-    if (piece < 0) return;
-    const int tile = piece % tiles;
-    const int outer0 = tile / a.inner_tiles * kLeft, inner0 = tile % a.inner_tiles * kRight;
-    const RowTile t = locate<true>(a.groups, a.chunk, 1, piece / tiles, lane);
+    Pieces pieces(count_tiles(a.groups, a.chunk, 1, lane) * tiles);
+    int outer0, inner0;
+    RowTile t;
+    auto place = [&](int piece, int& outer, int& inner, RowTile& chunk) {
+        const int tile = piece % tiles;
+        outer = tile / a.inner_tiles * kLeft;
+        inner = tile % a.inner_tiles * kRight;
+        chunk = locate<true>(a.groups, a.chunk, 1, piece / tiles, lane);
+    };
+    const int first = pieces.take();
+    if (first < 0) return;
+    place(first, outer0, inner0, t);
 
-    v16f acc[4][2];
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
     WideTile<false, kLeft> lt;
     WideTile<false, kRight> rt;
     lt.begin(a.left_stride, wave, lane);
     rt.begin(a.right_stride, wave, lane);
-    int rows = t.hi - t.lo;
-    const int rounds = (rows + kDepth - 1) / kDepth;
-    const uint16_t* left = reinterpret_cast<const uint16_t*>(a.left) + (int64_t)t.lo * a.left_stride + outer0;
-    const uint16_t* right = reinterpret_cast<const uint16_t*>(a.right) + (PACKED ? 0 : (int64_t)t.lo * a.right_stride + inner0);
-    int64_t row8 = t.lo + (tid >> 3);
-    const int col8 = inner0 + 32 * (tid & 7);
+    int rows, inner_now, outer_now, hi, col8;
+    int64_t row8;
+    const uint16_t *left, *right;
     typename Factor8::Pointer packed;
     packed.p = reinterpret_cast<const int8_t*>(a.right);
     packed.e = a.right_e;
     packed.stride = a.right_stride;
     typename Factor8::Raw raw[4];
+    auto begin = [&]() {
+        rows = t.hi - t.lo;
+        hi = t.hi;
+        outer_now = a.outer - outer0;
+        inner_now = a.inner - inner0;
+        left = reinterpret_cast<const uint16_t*>(a.left) + (int64_t)t.lo * a.left_stride + outer0;
+        right = reinterpret_cast<const uint16_t*>(a.right) + (PACKED ? 0 : (int64_t)t.lo * a.right_stride + inner0);
+        row8 = t.lo + (tid >> 3);
+        col8 = inner0 + 32 * (tid & 7);
+    };
     auto fetch = [&](unsigned char* l, unsigned char* r, bool more) {
-        lt.load(left, more ? ((int64_t)(rows - 1) * a.left_stride + a.outer - outer0) * 2 : 0, l, wave);
+        lt.load(left, more ? ((int64_t)(rows - 1) * a.left_stride + outer_now) * 2 : 0, l, wave);
         if (PACKED) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) raw[q] = Factor8::load(packed, row8, col8 + 8 * q, more && row8 < t.hi ? a.inner - (col8 + 8 * q) : 0);
+            for (int q = 0; q < 4; ++q) raw[q] = Factor8::load(packed, row8, col8 + 8 * q, more && row8 < hi ? a.inner - (col8 + 8 * q) : 0);
             row8 += kDepth;
         } else {
-            rt.load(right, more ? ((int64_t)(rows - 1) * a.right_stride + a.inner - inner0) * 2 : 0, r, wave);
+            rt.load(right, more ? ((int64_t)(rows - 1) * a.right_stride + inner_now) * 2 : 0, r, wave);
             right += (int64_t)kDepth * a.right_stride;
         }
         left += (int64_t)kDepth * a.left_stride;
@@ -218,13 +259,39 @@ __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
             *reinterpret_cast<u32x4*>(r + line * (kRight * 2) + (((4 * (tid & 7) + q) ^ RightTile::across(line)) << 4)) = v[0];
         }
     };
-    contract<kHalf, LeftTile, RightTile>(rounds, fetch, land, stages, wo, wi, lane, acc);
-    store_sums<4, 2>(a, t, outer0 + 128 * wo, inner0 + 64 * wi, acc, lane);
+    begin();
+    fetch(left0, right0, rows > 0);
+    loaded();
+    for (;;) {
+        v16f acc[4][2];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
+        const RowTile now = t;
+        const int now_outer = outer0, now_inner = inner0, rounds = (now.hi - now.lo + kDepth - 1) / kDepth, next = pieces.take();
+        if (next >= 0) place(next, outer0, inner0, t);
+        contract<kHalf, LeftTile, RightTile>(rounds, fetch, land, stages, wo, wi, lane, acc);
+        if (next >= 0) {
+            begin();
+            fetch(left0, right0, rows > 0);
+            loaded();
+        }
+        store_sums<4, 2>(a, now, now_outer + 128 * wo, now_inner + 64 * wi, acc, lane);
+        if (next < 0) break;
+    }
+}
+
+// one workgroup a compute unit, as many on every XCD
+unsigned wide_blocks(int64_t pieces) {
+    const int64_t units = compute_units() / kXcds * kXcds, blocks = (pieces + kXcds - 1) / kXcds * kXcds;
+    return (unsigned)(units > 0 && units < blocks ? units : blocks);
 }
 
 }  // namespace
 
-void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st) {
+void launch_wide_sums(int dtype, bool packed, const SumArgs& a, int64_t pieces, hipStream_t st) {
+    const unsigned grid = wide_blocks(pieces);
     if (dtype == kTypeF16) {
         if (packed) wide_sums_kernel<kTypeF16, true><<<grid, kThreads, 0, st>>>(a);
         else wide_sums_kernel<kTypeF16, false><<<grid, kThreads, 0, st>>>(a);
@@ -237,9 +304,9 @@ void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, h
 int launch_wide_rows(int dtype, bool backward, const RowsArgs& args, hipStream_t st) {
     RowsArgs a = args;
     a.col_tiles = (a.cols + kLeft - 1) / kLeft;
-    const int64_t blocks = (row_tiles(a.groups, kRight) * a.col_tiles + kXcds - 1) / kXcds * kXcds;
-    NEUS2_TRY(check_grid(blocks));
-    const unsigned grid = (unsigned)blocks;
+    const int64_t pieces = row_tiles(a.groups, kRight) * a.col_tiles;
+    NEUS2_TRY(check_grid(pieces));
+    const unsigned grid = a.rank > 0 ? (unsigned)((pieces + kXcds - 1) / kXcds * kXcds) : wide_blocks(pieces);
     if (dtype == kTypeF16) backward ? launch<kTypeF16, true>(a, grid, st) : launch<kTypeF16, false>(a, grid, st);
     else backward ? launch<kTypeBF16, true>(a, grid, st) : launch<kTypeBF16, false>(a, grid, st);
     return check_launch("wide layer");
