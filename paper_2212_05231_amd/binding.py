@@ -169,8 +169,9 @@ def _ptr_array(ts: Sequence):
 
 
 def _stream() -> int:
+    """The current stream of the current device, without the object torch.cuda.current_stream() makes of it (4 us a call)."""
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def validate_config(c: Neus2Config) -> int:
@@ -367,29 +368,36 @@ def _dtype_of(t) -> int:
 
 
 def _check_tensor(t, name, shape, dtype, device) -> None:
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, expected {tuple(shape)} of {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the rows are on device {device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
 
 
 def _check_rows(t, name, n, dim, stride, dtype, device) -> None:
     """[n, dim] with rows `stride` values apart (0: dim)."""
-    if tuple(t.shape) != (n, dim) or t.dtype != dtype:
+    if t.shape != (n, dim) or t.dtype != dtype:
         raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, expected {(n, dim)} of {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if n > 0 and dim > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) != (stride or dim):
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the rows are on device {device}")
+    if t.stride() != (stride or dim, 1) and (n > 0 and dim > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) != (stride or dim)):
         raise ValueError(f"{name}: strides {t.stride()}, expected {(stride or dim, 1)}")
 
 
-def _current_device(t, name):
+def _current_device(t, name) -> int:
+    """The device of a call's rows: the current one, or -1 for host memory, which _device_rows refuses once the shapes are right."""
     import torch
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
+    device = t.get_device()
+    if device >= 0 and device != torch.cuda.current_device():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return t.device
+    return device
+
+
+def _device_rows(device) -> None:
+    if device < 0:
+        raise ValueError("the rows are in host memory")
 
 
 def _layer_dtype(layer):
@@ -434,6 +442,7 @@ def grouped_fwd(layer, x, W, offsets, y) -> None:
     _check_tensor(W, "W", (layer.groups, layer.out_dim, layer.in_dim), dtype, device)
     _check_offsets(layer, offsets, device)
     _check_rows(y, "y", n, layer.out_dim, layer.y_stride, dtype, device)
+    _device_rows(device)
     _check(lib().neus2_grouped_fwd(C.byref(layer), _data(x), _data(W), _data(offsets), n, _data(y), _stream()))
 
 
@@ -455,6 +464,7 @@ def grouped_bwd(layer, x, W, offsets, dy, dx, dW, workspace=None, masks=None) ->
         _check_rows(dx, "dx", n, layer.in_dim, layer.x_stride, dtype, device)
     if dW is not None:
         _check_tensor(dW, "dW", (layer.groups, layer.out_dim, layer.in_dim), torch.float32, device)
+    _device_rows(device)
     _check(lib().neus2_grouped_bwd(C.byref(layer), xp, xq, xe, _data(masks), _data(W), _data(offsets), _data(dy), n, _data(dx),
                                    _data(dW), _ptr(workspace), _bytes(workspace), _stream()))
 
@@ -478,6 +488,7 @@ def adapter_fwd(layer, x, W, A, B, scales, slots, offsets, u, y) -> None:
     _check_bank(layer, A, B, scales, slots, offsets, device)
     _check_tensor(u, "u", (n, layer.rank), torch.float32, device)
     _check_rows(y, "y", n, layer.out_dim, layer.y_stride, dtype, device)
+    _device_rows(device)
     _check(lib().neus2_adapter_fwd(C.byref(layer), _data(x), _data(W), _data(A), _data(B), _data(scales), _data(slots), _data(offsets),
                                    n, _data(u), _data(y), _stream()))
 
@@ -503,6 +514,7 @@ def adapter_bwd(layer, x, W, A, B, scales, slots, offsets, u, dy, dx, dA, dB, wo
     for t, name, like in ((dA, "dA", A), (dB, "dB", B)):
         if t is not None:
             _check_tensor(t, name, like.shape, torch.float32, device)
+    _device_rows(device)
     _check(lib().neus2_adapter_bwd(C.byref(layer), xp, xq, xe, _data(masks), _data(W), _data(A), _data(B), _data(scales), _data(slots),
                                    _data(offsets), _data(u), _data(dy), n, _data(dx), _data(dA), _data(dB), _ptr(workspace),
                                    _bytes(workspace), _stream()))
@@ -524,6 +536,7 @@ def pack8(x, q, e, masks=None) -> None:
     device, (n, dim) = _current_device(x, "x"), x.shape
     _check_rows(x, "x", n, dim, x.stride(0) if n > 1 else 0, x.dtype, device)
     _check_packed_form(q, e, masks, n, dim, device)
+    _device_rows(device)
     _check(lib().neus2_pack8(_dtype_of(x), _data(x), x.stride(0) if n > 1 else 0, n, dim, _data(q), _data(e), _data(masks), _stream()))
 
 
@@ -531,6 +544,7 @@ def unpack8(q, e, x) -> None:
     device, (n, dim) = _current_device(x, "x"), x.shape
     _check_rows(x, "x", n, dim, x.stride(0) if n > 1 else 0, x.dtype, device)
     _check_packed_form(q, e, None, n, dim, device)
+    _device_rows(device)
     _check(lib().neus2_unpack8(_dtype_of(x), _data(q), _data(e), n, dim, _data(x), x.stride(0) if n > 1 else 0, _stream()))
 
 

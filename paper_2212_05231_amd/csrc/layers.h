@@ -162,23 +162,49 @@ __device__ __forceinline__ void split8(f32x8 v, u32x4 (&out)[TERMS]) {
     }
 }
 
+// Loads go through a window: an address range that begins at a uniform place and ends behind the last value that may be read.  A
+// lane that has nothing to read gives an offset outside, and gets zeros without a branch around the load (with branches, every load
+// waited for some forty scalar instructions).  Only whole units are read this way: `whole` in a factor's pointer says that memory
+// rows begin on 16 bytes, are a multiple of eight values long, and no more than 2^20 values apart.  Otherwise values are read one by one.
+constexpr uint32_t kOutside = 0x80000000u;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_window(const void* from, int64_t bytes) {
+    const int room = (int)(bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : bytes);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, room, 0x00020000);
+}
+
+__device__ __forceinline__ u32x4 window16(__amdgpu_buffer_rsrc_t w, uint32_t offset) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w, (int)offset, 0, 0));
+}
+
+// eight values from a place on 16 bytes, as floats
+__device__ __forceinline__ f32x8 eight(const float* p) {
+    const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ f32x8 eight(const _Float16* p) { return __builtin_convertvector(*reinterpret_cast<const h8*>(p), f32x8); }
+__device__ __forceinline__ f32x8 eight(const __bf16* p) { return __builtin_convertvector(*reinterpret_cast<const bf8*>(p), f32x8); }
+
 // 16-bit values as they are
 struct Native {
     struct Raw { u32x4 v; };
-    struct Pointer { const uint16_t* p; int64_t stride; int vec; };
+    struct Pointer { const uint16_t* p; int64_t stride; int whole; };
+    struct Window { __amdgpu_buffer_rsrc_t r; uint32_t stride; };
     static constexpr int kTerms = 1;
+    // rows and length: how many memory rows there are from `row` on, and how many values in a row from `col` on
+    __device__ static __forceinline__ Window window(const Pointer& f, int64_t row, int64_t col, int rows, int64_t length) {
+        return {make_window(f.p + row * f.stride + col, rows > 0 ? ((rows - 1) * f.stride + length) * 2 : 0), (uint32_t)f.stride * 2u};
+    }
+    __device__ static __forceinline__ Raw fetch(const Window& w, int row, int col, bool in) {
+        return {window16(w.r, in ? (uint32_t)row * w.stride + (uint32_t)col * 2u : kOutside)};
+    }
     __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) {
         Raw r;
         r.v = zero4();
-        if (valid <= 0) return r;
         const uint16_t* p = f.p + row * f.stride + col;
-        if (valid >= 8 && f.vec) {
-            r.v = *reinterpret_cast<const u32x4*>(p);
-        } else {
 #pragma unroll
-            for (int s = 0; s < 8; ++s)
-                if (s < valid) r.v[s >> 1] |= (uint32_t)p[s] << (16 * (s & 1));
-        }
+        for (int s = 0; s < 8; ++s)
+            if (s < valid) r.v[s >> 1] |= (uint32_t)p[s] << (16 * (s & 1));
         return r;
     }
     __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[1]) { out[0] = r.v; }
@@ -188,22 +214,22 @@ struct Native {
 template <int TERMS>
 struct Wide {
     struct Raw { f32x8 v; };
-    struct Pointer { const float* p; int64_t stride; int vec; };
+    struct Pointer { const float* p; int64_t stride; int whole; };
+    struct Window { __amdgpu_buffer_rsrc_t r; uint32_t stride; };
     static constexpr int kTerms = TERMS;
+    __device__ static __forceinline__ Window window(const Pointer& f, int64_t row, int64_t col, int rows, int64_t length) {
+        return {make_window(f.p + row * f.stride + col, rows > 0 ? ((rows - 1) * f.stride + length) * 4 : 0), (uint32_t)f.stride * 4u};
+    }
+    __device__ static __forceinline__ Raw fetch(const Window& w, int row, int col, bool in) {
+        const uint32_t at = in ? (uint32_t)row * w.stride + (uint32_t)col * 4u : kOutside;
+        const v4f a = __builtin_bit_cast(v4f, window16(w.r, at)), b = __builtin_bit_cast(v4f, window16(w.r, at + 16u));
+        return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+    }
     __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) {
         Raw r;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) r.v[s] = 0.f;
-        if (valid <= 0) return r;
         const float* p = f.p + row * f.stride + col;
-        if (valid >= 8 && f.vec) {
-            const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
-            r.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else {
 #pragma unroll
-            for (int s = 0; s < 8; ++s)
-                if (s < valid) r.v[s] = p[s];
-        }
+        for (int s = 0; s < 8; ++s) r.v[s] = s < valid ? p[s] : 0.f;
         return r;
     }
     __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[TERMS]) { split8<TERMS>(r.v, out); }
@@ -213,7 +239,12 @@ struct Wide {
 struct HalfPair {
     typedef Native::Raw Raw;
     typedef Native::Pointer Pointer;
+    typedef Native::Window Window;
     static constexpr int kTerms = 2;
+    __device__ static __forceinline__ Window window(const Pointer& f, int64_t row, int64_t col, int rows, int64_t length) {
+        return Native::window(f, row, col, rows, length);
+    }
+    __device__ static __forceinline__ Raw fetch(const Window& w, int row, int col, bool in) { return Native::fetch(w, row, col, in); }
     __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) { return Native::load(f, row, col, valid); }
     __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[2]) {
         split8<2>(__builtin_convertvector(__builtin_bit_cast(h8, r.v), f32x8), out);
@@ -223,22 +254,25 @@ struct HalfPair {
 __device__ __forceinline__ float signed_byte(uint32_t word, int byte) { return (float)((int)(word << (24 - 8 * byte)) >> 24); }
 
 // 8-bit values with an exponent per 32 of them (neus2_pack8), as bf16 or fp16: q 2^(e-127) has at most 7 significant bits,
-// exact in both.  e = 255 marks a block that held a value that was not finite: 0 * inf = NaN.
+// exact in both.  e = 255 marks a block that held a value that was not finite: 0 * inf = NaN.  Its rows are always whole.
 template <bool HALF>
 struct Packed {
     struct Raw { uint32_t q[2]; uint32_t e; };
-    struct Pointer { const int8_t* p; const uint8_t* e; int64_t stride; };     // stride: 32 * blocks
+    struct Pointer { const int8_t* p; const uint8_t* e; int64_t stride; int whole; };     // stride: 32 * blocks
+    struct Window { __amdgpu_buffer_rsrc_t q, e; uint32_t stride; };
     static constexpr int kTerms = 1;
-    __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) {
-        Raw r = {{0u, 0u}, 0u};
-        if (valid <= 0) return r;
-        const int64_t at = row * f.stride + col;                               // behind the last column the packed form holds zeros
-        const uint2 w = *reinterpret_cast<const uint2*>(f.p + at);
-        r.q[0] = w.x;
-        r.q[1] = w.y;
-        r.e = f.e[at >> 5];
-        return r;
+    // col is a multiple of 32
+    __device__ static __forceinline__ Window window(const Pointer& f, int64_t row, int64_t col, int rows, int64_t) {
+        const int64_t at = row * f.stride + col, bytes = rows > 0 ? rows * f.stride - col : 0;
+        return {make_window(f.p + at, bytes), make_window(f.e + (at >> 5), bytes >> 5), (uint32_t)f.stride};
     }
+    __device__ static __forceinline__ Raw fetch(const Window& w, int row, int col, bool in) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const uint32_t at = (uint32_t)row * w.stride + (uint32_t)col;
+        const u32x2 q = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(w.q, (int)(in ? at : kOutside), 0, 0));
+        return {{q[0], q[1]}, __builtin_amdgcn_raw_buffer_load_b8(w.e, (int)(in ? at >> 5 : kOutside), 0, 0)};
+    }
+    __device__ static __forceinline__ Raw load(const Pointer&, int64_t, int, int) { return {{0u, 0u}, 0u}; }
     __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[1]) {
         typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
         typedef _Float16 h2 __attribute__((ext_vector_type(2)));
@@ -279,15 +313,23 @@ struct FactorTile {
     __device__ static __forceinline__ int across(int k) { return across_swizzle<LINES>(k); }
     __device__ static __forceinline__ int swizzle(int line) { return DEPTH == 64 ? (line >> 1) & 7 : (line >> 2) & 3; }
 
-    // lines0, step0: where the tile begins; lines, steps: how many there are in all (the rest is zero)
+    // line0, step0: where the tile begins; lines, steps: how many there are from there on (the rest is zero)
     __device__ __forceinline__ void load(const typename Factor::Pointer& f, int64_t line0, int lines, int64_t step0, int steps, int tid) {
+        const int rows = ALONG ? min(lines, LINES) : min(steps, DEPTH), length = ALONG ? steps : lines;
+        if (f.whole) {
+            const typename Factor::Window w = Factor::window(f, ALONG ? line0 : step0, ALONG ? step0 : line0, rows, length);
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int unit = tid + k * THREADS;
-            const int r = unit / kPieces, c = unit % kPieces * 8;
-            const bool in = kUnits % THREADS == 0 || unit < kUnits;
-            if (ALONG) raw[k] = Factor::load(f, line0 + r, (int)step0 + c, in && r < lines ? steps - c : 0);
-            else raw[k] = Factor::load(f, step0 + r, (int)line0 + c, in && r < steps ? lines - c : 0);
+            for (int k = 0; k < kPer; ++k) {
+                const int unit = tid + k * THREADS, r = unit / kPieces, c = unit % kPieces * 8;
+                raw[k] = Factor::fetch(w, r, c, r < rows && c < length && (kUnits % THREADS == 0 || unit < kUnits));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const int unit = tid + k * THREADS, r = unit / kPieces, c = unit % kPieces * 8;
+                const bool in = r < rows && (kUnits % THREADS == 0 || unit < kUnits);
+                raw[k] = Factor::load(f, (ALONG ? line0 : step0) + r, (int)(ALONG ? step0 : line0) + c, in ? length - c : 0);
+            }
         }
     }
     __device__ __forceinline__ void store(unsigned char* __restrict__ lds, int tid) const {
@@ -372,8 +414,8 @@ __device__ __forceinline__ int slot_of(const int32_t* __restrict__ slots, int n_
 
 struct RowsArgs {
     RowGroups groups;
-    const void* x; int64_t x_stride; int x_vec;            // the data rows: x forward, dy backward
-    const void* w; int64_t w_group; int w_stride, w_vec;   // matrix of group g at w + g * w_group, memory rows of w_stride values
+    const void* x; int64_t x_stride; int x_whole;          // the data rows: x forward, dy backward
+    const void* w; int64_t w_group; int w_stride, w_whole; // matrix of group g at w + g * w_group, memory rows of w_stride values
     int steps;                                             // length of the contraction
     int cols;                                              // outputs per row
     void* y; int64_t y_stride; int y_vec;
@@ -392,41 +434,60 @@ template <int DT> struct AdapterTerms {
     static constexpr int kBank = DT == kTypeF32 ? 3 : DT == kTypeF16 ? 2 : 1;
 };
 
-// eight values of a row (k .. k + 7 of `rank`) as floats, zero where the row counts for nothing
-__device__ __forceinline__ f32x8 load_u(const float* __restrict__ u, int64_t row, int rank, int k, bool counts) {
+// eight values of row `row` (k .. k + 7 of `rank`) of a window over u, zeros where the row counts for nothing
+__device__ __forceinline__ f32x8 load_u(__amdgpu_buffer_rsrc_t u, int row, int rank, int k, bool counts) {
     f32x8 v;
+    const uint32_t at = (uint32_t)(row * rank + k) * 4u;
+    if ((rank & 7) == 0) {
+        const bool in = counts && k < rank;
+        const v4f a = __builtin_bit_cast(v4f, window16(u, in ? at : kOutside)), b = __builtin_bit_cast(v4f, window16(u, in ? at + 16u : kOutside));
+        v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
 #pragma unroll
-    for (int s = 0; s < 8; ++s) v[s] = 0.f;
-    if (!counts) return v;
-    const float* p = u + row * rank + k;
-    if ((rank & 7) == 0 && k < rank) {
-        const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int s = 0; s < 8; ++s)
+            v[s] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(u, (int)(counts && k + s < rank ? at + 4u * s : kOutside), 0, 0));
     }
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-        if (k + s < rank) v[s] = p[s];
     return v;
 }
 
-// eight values bank(col, k .. k + 7): along the memory row forward (bank [col][rank]), down the column backward ([rank][cols])
+template <int DT>
+__device__ __forceinline__ float window_value(__amdgpu_buffer_rsrc_t w, uint32_t index, bool in) {
+    typedef typename TypeOf<DT>::Element E;
+    if constexpr (DT == kTypeF32) return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(w, (int)(in ? index * 4u : kOutside), 0, 0));
+    else return (float)__builtin_bit_cast(E, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(w, (int)(in ? index * 2u : kOutside), 0, 0));
+}
+
+// eight values bank(col, k .. k + 7) of a window over one adapter's matrix: along the memory row forward (bank [col][rank]), down the
+// column backward ([rank][cols])
 template <int DT, bool BACKWARD>
-__device__ __forceinline__ f32x8 load_bank(const typename TypeOf<DT>::Element* __restrict__ bank, int rank, int cols, int col, int k) {
+__device__ __forceinline__ f32x8 load_bank(__amdgpu_buffer_rsrc_t bank, int rank, int cols, int col, int k) {
+    typedef typename TypeOf<DT>::Element E;
     f32x8 v;
+    if (!BACKWARD && (rank & 7) == 0) {
+        const uint32_t at = (uint32_t)(col * rank + k) * (uint32_t)sizeof(E);
+        const bool in = col < cols && k < rank;
+        const u32x4 a = window16(bank, in ? at : kOutside);
+        if constexpr (DT == kTypeF32) {
+            const v4f b = __builtin_bit_cast(v4f, window16(bank, in ? at + 16u : kOutside));
+            v = __builtin_shufflevector(__builtin_bit_cast(v4f, a), b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else if constexpr (DT == kTypeF16) {
+            v = __builtin_convertvector(__builtin_bit_cast(h8, a), f32x8);
+        } else {
+            v = __builtin_convertvector(__builtin_bit_cast(bf8, a), f32x8);
+        }
+    } else {
 #pragma unroll
-    for (int s = 0; s < 8; ++s) v[s] = 0.f;
-    if (col >= cols) return v;
-    if (!BACKWARD && (rank & 7) == 0 && k < rank) {
-        typedef typename TypeOf<DT>::Element E;
-        typedef E E4 __attribute__((ext_vector_type(4)));
-        const E* p = bank + (int64_t)col * rank + k;
-        const E4 a = *reinterpret_cast<const E4*>(p), b = *reinterpret_cast<const E4*>(p + 4);
-        return __builtin_convertvector(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), f32x8);
+        for (int s = 0; s < 8; ++s)
+            v[s] = window_value<DT>(bank, (uint32_t)(BACKWARD ? (k + s) * cols + col : col * rank + k + s), col < cols && k + s < rank);
     }
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-        if (k + s < rank) v[s] = (float)(BACKWARD ? bank[(int64_t)(k + s) * cols + col] : bank[(int64_t)col * rank + k + s]);
     return v;
+}
+
+template <int DT>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bank_window(const void* bank, int slot, int rank, int cols) {
+    typedef typename TypeOf<DT>::Element E;
+    const int64_t size = (int64_t)rank * cols;
+    return make_window(reinterpret_cast<const E*>(bank) + slot * size, size * (int64_t)sizeof(E));
 }
 
 // What follows the contraction, for one wave's kBC x kBR blocks of 32 outputs (from col0 on) and 32 rows (from t.lo + row0 on).  A
@@ -443,19 +504,20 @@ __device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t,
         // y += bank[slot] u, segment after segment: operands straight from memory (a lane's eight values lie together), the rows of
         // other segments zero.  A tile inside one segment takes rank / 16 more k-steps.
         constexpr int kU = AdapterTerms<DT>::kU, kBank = AdapterTerms<DT>::kBank;
+        const __amdgpu_buffer_rsrc_t us = make_window(a.u + (int64_t)t.lo * a.rank, (int64_t)(t.hi - t.lo) * a.rank * 4);
         int s = segment_of(a.segments, a.n_segments, t.lo, lane);
         for (; s < a.n_segments; ++s) {
             const int lo = max(a.segments[s], t.lo), hi = min(a.segments[s + 1], t.hi);
             if (lo >= t.hi) break;
             const int slot = hi > lo ? slot_of(a.slots, a.n_slots, s) : -1;
             if (slot < 0) continue;
-            const E* bank = reinterpret_cast<const E*>(a.bank) + (int64_t)slot * a.rank * a.cols;
+            const __amdgpu_buffer_rsrc_t bank = bank_window<DT>(a.bank, slot, a.rank, a.cols);
             for (int k0 = 0; k0 < a.rank; k0 += 16) {
                 u32x4 u[kBR][kU];
 #pragma unroll
                 for (int r = 0; r < kBR; ++r) {
                     const int row = t.lo + row0 + 32 * r + j;
-                    split8<kU>(load_u(a.u, row, a.rank, k0 + 8 * h, row >= lo && row < hi), u[r]);
+                    split8<kU>(load_u(us, row - t.lo, a.rank, k0 + 8 * h, row >= lo && row < hi), u[r]);
                 }
 #pragma unroll
                 for (int c = 0; c < kBC; ++c) {
@@ -522,8 +584,8 @@ __device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t,
 struct SumArgs {
     RowGroups groups;
     int chunk;                       // rows a workgroup sums over
-    const void* left; int64_t left_stride; int left_vec;
-    const void* right; const uint8_t* right_e; int64_t right_stride; int right_vec;
+    const void* left; int64_t left_stride; int left_whole;
+    const void* right; const uint8_t* right_e; int64_t right_stride; int right_whole;
     int outer, inner;
     float* out; int accumulate;
     float* partial;                  // [partials][outer][inner]: sums of chunks, of all of them (by_slot) or of those that share a group
@@ -568,7 +630,7 @@ __device__ __forceinline__ void store_sums(const SumArgs& a, const RowTile& t, i
 }
 
 constexpr int kWideOuter = 256, kWideInner = 256;       // their tiles
-void launch_wide_sums(int dtype, bool packed, const SumArgs& a, int64_t pieces, hipStream_t st);
+void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st);
 int launch_wide_rows(int dtype, bool backward, const RowsArgs& a, hipStream_t st);      // 16-bit types, whole lines of the contraction
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------
@@ -592,6 +654,9 @@ inline int element_bytes(int dtype) { return dtype == kTypeF32 ? 4 : 2; }
 
 // rows of `stride` values begin on 16-byte boundaries
 inline int rows_aligned(int dtype, int64_t stride) { return (stride * element_bytes(dtype)) % 16 == 0; }
+
+// ... and are read in whole units of eight values, through 32-bit offsets
+inline int rows_whole(int dtype, int64_t stride, int64_t length) { return rows_aligned(dtype, stride) && length % 8 == 0 && stride <= (1 << 20); }
 
 inline int64_t row_tiles(const RowGroups& g, int rows) {
     return ((int64_t)g.n + rows - 1) / rows + (g.offsets && !g.whole ? g.groups : 0);

@@ -32,10 +32,10 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
     typename Factor::Pointer data, matrix;
     data.p = reinterpret_cast<decltype(data.p)>(a.x);
     data.stride = a.x_stride;
-    data.vec = a.x_vec;
+    data.whole = a.x_whole;
     matrix.p = reinterpret_cast<decltype(matrix.p)>(a.w) + (int64_t)t.group * a.w_group;
     matrix.stride = a.w_stride;
-    matrix.vec = a.w_vec;
+    matrix.whole = a.w_whole;
     DataTile dt;
     MatrixTile mt;
     v16f acc[kBC][kBR];
@@ -88,25 +88,24 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------
 // 16 rows and 16 outputs on the 16x16x32 instruction, operands straight from memory: with so few rows the pass is bound by reading
-// the matrices once, and there is nothing to share through LDS.  A lane reads 32 consecutive bytes of a matrix row, four lanes a
-// whole line.  SPLIT: the four waves of a workgroup share the contraction (their sums are joined in LDS); otherwise every wave has 16
-// rows of its own.  TO_U: the low-rank products u = scale A x and v = scale B^T dy of adapters, in fp32, every segment with the
-// matrix of its slot (rows of a segment without one get zeros).  DOWN: the contraction runs down the matrix's columns (B^T dy).
+// the matrices once, and there is nothing to share through LDS.  The eight waves of a workgroup share the contraction, each with up to
+// four lines of every matrix row in flight (2048 steps of a 16-bit type at once); four lanes read a line's 64 bytes.  Their sums are
+// joined in LDS, and a thread adds what the row's adapter gives.
 struct FewArgs {
     RowGroups groups;
-    const void* x; int64_t x_stride; int x_vec;
-    const void* w; int64_t w_group; int w_stride, w_vec;
+    const void* x; int64_t x_stride; int x_whole;
+    const void* w; int64_t w_group; int w_stride, w_whole;
     int steps, cols;
     void* y; int64_t y_stride;
     int relu;
-    const int32_t* slots; int n_slots; const float* scales;       // TO_U
-    const int32_t* segments; int n_segments;                      // !TO_U with adapters
-    const float* u; const void* bank; int rank;
+    const int32_t* segments; int n_segments; const int32_t* slots; int n_slots; const float* u; const void* bank; int rank;
     int col_tiles;
 };
 
-template <int DT, bool TO_U, bool DOWN, bool SPLIT>
-__global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a) {
+constexpr int kFewWaves = 8;
+
+template <int DT>
+__global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewArgs a) {
     typedef typename TypeOf<DT>::Element E;
     typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
     constexpr int kTerms = Factor::kTerms;
@@ -114,114 +113,214 @@ __global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a) {
     constexpr int kUnits = DT == kTypeF32 ? 1 : 2;            // operands a lane takes of one line of 128 bytes
     constexpr int kChunk = 32 * kUnits;                       // steps of the contraction they cover
     constexpr int kAhead = 4;
-    constexpr int kRows = SPLIT ? 16 : 64;
-    __shared__ v4f part[SPLIT ? 4 : 1][64];
+    __shared__ v4f part[kFewWaves][64];
     __shared__ int row_slot[16];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col0 = (int)(blockIdx.x % a.col_tiles) * 16;
-    RowTile t = locate(a.groups, kRows, 0, (int)(blockIdx.x / a.col_tiles), lane);
+    const RowTile t = locate(a.groups, 16, 0, (int)(blockIdx.x / a.col_tiles), lane);
     if (t.group < 0) return;
-    if (!SPLIT) {
-        t.lo += 16 * wave;
-        if (t.lo >= t.hi) return;
-    }
-    int slot = t.group;
-    if (TO_U) slot = slot_of(a.slots, a.n_slots, t.group);
 
     const int i = lane & 15, quarter = lane >> 4;
     v4f acc = {0.f, 0.f, 0.f, 0.f};
-    if (slot >= 0) {
-        typename Factor::Pointer data, matrix;
-        data.p = reinterpret_cast<decltype(data.p)>(a.x);
-        data.stride = a.x_stride;
-        data.vec = a.x_vec;
-        matrix.p = reinterpret_cast<decltype(matrix.p)>(a.w) + (int64_t)slot * a.w_group;
-        matrix.stride = a.w_stride;
-        matrix.vec = a.w_vec;
-        const bool row_in = t.lo + i < t.hi, col_in = col0 + i < a.cols;
-        const int stride = (SPLIT ? 4 : 1) * kChunk;
-        for (int base = SPLIT ? wave * kChunk : 0; base < a.steps; base += kAhead * stride) {
-            typename Factor::Raw w[kAhead][kUnits], x[kAhead][kUnits];
+    typename Factor::Pointer data, matrix;
+    data.p = reinterpret_cast<decltype(data.p)>(a.x);
+    data.stride = a.x_stride;
+    data.whole = a.x_whole;
+    matrix.p = reinterpret_cast<decltype(matrix.p)>(a.w) + (int64_t)t.group * a.w_group;
+    matrix.stride = a.w_stride;
+    matrix.whole = a.w_whole;
+    const bool row_in = t.lo + i < t.hi, col_in = col0 + i < a.cols;
+    const typename Factor::Window xs = Factor::window(data, t.lo, 0, t.hi - t.lo, a.steps), ws = Factor::window(matrix, col0, 0, min(16, a.cols - col0), a.steps);
+    const bool whole = a.x_whole && a.w_whole;
+    // A wave's part of the contraction is one piece: rows that lie a power of two apart hang on the same memory channels, and waves
+    // that walk side by side would all be at the same few of them.
+    const int length = (a.steps + kFewWaves * kChunk - 1) / (kFewWaves * kChunk) * kChunk, end = min(a.steps, (wave + 1) * length);
+    for (int base = wave * length; base < end; base += kAhead * kChunk) {
+        typename Factor::Raw w[kAhead][kUnits], x[kAhead][kUnits];
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q)
+        for (int q = 0; q < kAhead; ++q)
 #pragma unroll
-                for (int v = 0; v < kUnits; ++v) {
-                    const int k = base + q * stride + 8 * kUnits * quarter + 8 * v;
-                    if (DOWN) {
-                        typename Factor::Raw& r = w[q][v];
-                        r.v = Factor::load(matrix, 0, 0, 0).v;
-                        const E* p = reinterpret_cast<const E*>(matrix.p) + (int64_t)k * a.w_stride + col0 + i;
-#pragma unroll
-                        for (int s = 0; s < 8; ++s)
-                            if (col_in && k + s < a.steps) {
-                                const E value = p[(int64_t)s * a.w_stride];
-                                if constexpr (DT == kTypeF32) r.v[s] = value;
-                                else r.v[s >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, value) << (16 * (s & 1));
-                            }
-                    } else {
-                        w[q][v] = Factor::load(matrix, col0 + i, k, col_in ? a.steps - k : 0);
-                    }
-                    x[q][v] = Factor::load(data, t.lo + i, k, row_in ? a.steps - k : 0);
+            for (int v = 0; v < kUnits; ++v) {
+                const int k = base + q * kChunk + 32 * v + 8 * quarter;
+                if (whole) {
+                    w[q][v] = Factor::fetch(ws, i, k, col_in && k < end);
+                    x[q][v] = Factor::fetch(xs, i, k, row_in && k < end);
+                } else {
+                    w[q][v] = Factor::load(matrix, col0 + i, k, col_in ? end - k : 0);
+                    x[q][v] = Factor::load(data, t.lo + i, k, row_in ? end - k : 0);
                 }
+            }
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q)
+        for (int q = 0; q < kAhead; ++q)
 #pragma unroll
-                for (int v = 0; v < kUnits; ++v) {
-                    u32x4 wt[kTerms], xt[kTerms];
-                    Factor::terms(w[q][v], wt);
-                    Factor::terms(x[q][v], xt);
+            for (int v = 0; v < kUnits; ++v) {
+                u32x4 wt[kTerms], xt[kTerms];
+                Factor::terms(w[q][v], wt);
+                Factor::terms(x[q][v], xt);
 #pragma unroll
-                    for (int p = 0; p < kTerms; ++p)
+                for (int p = 0; p < kTerms; ++p)
 #pragma unroll
-                        for (int r = 0; r < kTerms; ++r)
-                            if (p + r < kTerms) acc = mma16<kHalf>(wt[p], xt[r], acc);
-                }
-        }
+                    for (int r = 0; r < kTerms; ++r)
+                        if (p + r < kTerms) acc = mma16<kHalf>(wt[p], xt[r], acc);
+            }
     }
     // lane: row lane % 16, outputs 4 (lane / 16) .. + 3
-    if constexpr (SPLIT) {
-        if (!TO_U && a.rank > 0) {
+    if (a.rank > 0) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = min(t.lo + 4 * wave + r, t.hi - 1);
-                const int s = segment_of(a.segments, a.n_segments, row, lane);
-                const int of = s < a.n_segments ? slot_of(a.slots, a.n_slots, s) : -1;
-                if (lane == 0) row_slot[4 * wave + r] = of;
-            }
+        for (int r = 0; r < 16 / kFewWaves; ++r) {
+            const int of = 16 / kFewWaves * wave + r, s = segment_of(a.segments, a.n_segments, min(t.lo + of, t.hi - 1), lane);
+            const int slot = s < a.n_segments ? slot_of(a.slots, a.n_slots, s) : -1;
+            if (lane == 0) row_slot[of] = slot;
         }
-        part[wave][lane] = acc;
-        __syncthreads();
-        // a thread per output, the outputs of a row side by side
-        const int row = tid >> 4, c = tid & 15, col = col0 + c;
-        float z = 0.f;
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    // a thread per output, the outputs of a row side by side
+    const int row = tid >> 4, c = tid & 15, col = col0 + c;
+    const int64_t at = t.lo + row;
+    if (row >= 16 || at >= t.hi || col >= a.cols) return;
+    float z = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) z += part[w][(c >> 2) * 16 + row][c & 3];
-        const int64_t at = t.lo + row;
-        if (at >= t.hi || col >= a.cols) return;
-        if constexpr (TO_U) {
-            reinterpret_cast<float*>(a.y)[at * a.y_stride + col] = slot >= 0 ? z * a.scales[slot] : 0.f;
+    for (int w = 0; w < kFewWaves; ++w) z += part[w][(c >> 2) * 16 + row][c & 3];
+    if (a.rank > 0 && row_slot[row] >= 0) {
+        const E* bank = reinterpret_cast<const E*>(a.bank) + ((int64_t)row_slot[row] * a.cols + col) * a.rank;
+        const float* u = a.u + at * a.rank;
+        if (a.rank % 8 == 0) {
+            for (int k = 0; k < a.rank; k += 8) {
+                const f32x8 b = eight(bank + k), v = eight(u + k);
+#pragma unroll
+                for (int s = 0; s < 8; ++s) z += b[s] * v[s];
+            }
         } else {
-            if (a.rank > 0 && row_slot[row] >= 0) {
-                const E* bank = reinterpret_cast<const E*>(a.bank) + (int64_t)row_slot[row] * a.rank * a.cols;
-                for (int k = 0; k < a.rank; k += 8) {
-                    const f32x8 b = load_bank<DT, false>(bank, a.rank, a.cols, col, k), u = load_u(a.u, at, a.rank, k, true);
+            for (int k = 0; k < a.rank; ++k) z += (float)bank[k] * u[k];
+        }
+    }
+    reinterpret_cast<E*>(a.y)[at * a.y_stride + col] = (E)(a.relu ? relu1(z) : z);
+}
+
+// ---- the low-rank products of adapters -------------------------------------------------------------------------------------------
+// u = scale A[slot] x (DOWN = false) or v = scale B[slot]^T dy (DOWN = true: the contraction runs down the matrix's columns), fp32, zeros
+// for the rows of segments without a slot.  Bound by reading the rows, which are many and wide beside the few outputs: one workgroup
+// has all outputs of its 32 rows, so that they are read once (16 outputs a workgroup, the rows read once per 16: 8192 x 2048, rank 64,
+// 36 us).  SPLIT: the eight waves share the contraction; otherwise (short ones) every wave has 32 rows of its own.
+struct LowRankArgs {
+    RowGroups groups;
+    const void* x; int64_t x_stride; int x_whole;
+    const void* bank; int64_t bank_slot; int bank_whole;
+    int steps, rank;
+    const int32_t* slots; int n_slots; const float* scales;
+    float* u;
+};
+
+template <int DT, bool DOWN, bool SPLIT, int BLOCKS>
+__global__ __launch_bounds__(512) void low_rank_kernel(LowRankArgs a) {
+    typedef typename TypeOf<DT>::Element E;
+    typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
+    constexpr int kTerms = Factor::kTerms, kAhead = 4;        // k-steps whose operands are in flight together
+    constexpr bool kHalf = DT == kTypeF16;
+    constexpr int kWaves = 8;
+    __shared__ float part[SPLIT ? kWaves : 1][SPLIT ? BLOCKS * 32 : 1][33];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, (int)blockIdx.x, lane);
+    if (t.group < 0) return;
+    if (!SPLIT) {
+        t.lo += 32 * wave;
+        t.hi = min(t.hi, t.lo + 32);
+        if (t.lo >= t.hi) return;
+    }
+    const int slot = slot_of(a.slots, a.n_slots, t.group);
+    const int j = lane & 31, h = lane >> 5;
+    if (slot < 0) {
+        for (int i = SPLIT ? tid : lane; i < (t.hi - t.lo) * a.rank; i += SPLIT ? 512 : 64) a.u[(int64_t)t.lo * a.rank + i] = 0.f;
+        return;
+    }
+    typename Factor::Pointer data, matrix;
+    data.p = reinterpret_cast<decltype(data.p)>(a.x);
+    data.stride = a.x_stride;
+    data.whole = a.x_whole;
+    matrix.p = reinterpret_cast<decltype(matrix.p)>(a.bank) + (int64_t)slot * a.bank_slot;
+    matrix.stride = a.steps;
+    matrix.whole = a.bank_whole;
+    const bool row_in = t.lo + j < t.hi;
+    const typename Factor::Window xs = Factor::window(data, t.lo, 0, t.hi - t.lo, a.steps), bs = Factor::window(matrix, 0, 0, a.rank, a.steps);
+    const __amdgpu_buffer_rsrc_t down = make_window(matrix.p, a.bank_slot * (int64_t)sizeof(E));
+    const bool whole = a.x_whole && (DOWN || a.bank_whole);
+    v16f acc[BLOCKS];
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) z += b[s] * u[s];
+    for (int b = 0; b < BLOCKS; ++b) acc[b] = zero16();
+    constexpr int kRun = 16 * kAhead;
+    const int length = (a.steps + kWaves * kRun - 1) / (kWaves * kRun) * kRun;          // one piece for every wave, see above
+    const int end = SPLIT ? min(a.steps, (wave + 1) * length) : a.steps;
+    for (int base = SPLIT ? wave * length : 0; base < end; base += kRun) {
+        typename Factor::Raw x[kAhead], w[BLOCKS][kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int k = base + 16 * q + 8 * h;
+            if (whole) x[q] = Factor::fetch(xs, j, k, row_in && k < end);
+            else x[q] = Factor::load(data, t.lo + j, k, row_in ? end - k : 0);
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const int r = 32 * b + j;
+                if constexpr (DOWN) {
+                    // eight values below each other, of 32 columns side by side; their bits as they are
+                    uint32_t bits[8];
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const bool in = r < a.rank && k + s < end;
+                        const uint32_t at = (uint32_t)((k + s) * a.rank + r) * (uint32_t)sizeof(E);
+                        if constexpr (DT == kTypeF32) bits[s] = __builtin_amdgcn_raw_buffer_load_b32(down, (int)(in ? at : kOutside), 0, 0);
+                        else bits[s] = __builtin_amdgcn_raw_buffer_load_b16(down, (int)(in ? at : kOutside), 0, 0);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        if constexpr (DT == kTypeF32) w[b][q].v[s] = __builtin_bit_cast(float, bits[s]);
+                        else if (s % 2 == 0) w[b][q].v[s >> 1] = bits[s] | bits[s + 1] << 16;
+                    }
+                } else if (whole) {
+                    w[b][q] = Factor::fetch(bs, r, k, r < a.rank && k < end);
+                } else {
+                    w[b][q] = Factor::load(matrix, r, k, r < a.rank ? end - k : 0);
                 }
             }
-            reinterpret_cast<E*>(a.y)[at * a.y_stride + col] = (E)(a.relu ? relu1(z) : z);
         }
-    } else {
-        static_assert(SPLIT || TO_U, "rows of their own: the low-rank products only");
-        const int64_t at = t.lo + i;
-        if (at >= t.hi) return;
-        const float scale = slot >= 0 ? a.scales[slot] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int col = col0 + 4 * quarter + e;
-            if (col < a.cols) reinterpret_cast<float*>(a.y)[at * a.y_stride + col] = slot >= 0 ? acc[e] * scale : 0.f;
+        for (int q = 0; q < kAhead; ++q) {
+            u32x4 xt[kTerms], wt[kTerms];
+            Factor::terms(x[q], xt);
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                Factor::terms(w[b][q], wt);
+                acc[b] = mma_terms<kHalf>(wt, xt, acc[b]);
+            }
         }
+    }
+    // lane: row j, outputs 32 b + neuron_of(r, h)
+    const float scale = a.scales[slot];
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) part[wave][32 * b + neuron_of(r, h)][j] = acc[b][r];
+        __syncthreads();
+        for (int i = tid; i < 32 * a.rank; i += 512) {
+            const int row = i / a.rank, r = i - row * a.rank;
+            if (t.lo + row >= t.hi) break;
+            float z = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) z += part[w][r][row];
+            a.u[(int64_t)t.lo * a.rank + i] = z * scale;
+        }
+    } else if (row_in) {
+        float* out = a.u + (int64_t)(t.lo + j) * a.rank;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int at = 32 * b + neuron_of(r, h);
+                if (at < a.rank) out[at] = acc[b][r] * scale;
+            }
     }
 }
 
@@ -230,7 +329,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a) {
 // which it rounds to at most 127 steps of 2^t (t >= -126).  All of it is exact: x 2^-t is a change of exponent, the rounding to whole
 // steps (ties to even) the only one.  Bound by the memory: 4 or 2 bytes read, 1.03 (1.16 with masks) written a feature.
 template <int DT>
-__global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ x, int64_t x_stride, int vec, int64_t n, int dim,
+__global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ x, int64_t x_stride, int whole, int64_t n, int dim,
                                                    int8_t* __restrict__ q, uint8_t* __restrict__ e, uint32_t* __restrict__ masks) {
     typedef std::conditional_t<DT == kTypeF32, Wide<1>, Native> Factor;
     const int units = (dim + 31) / 32 * 4;
@@ -238,17 +337,21 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ x, i
     typename Factor::Pointer f;
     f.p = reinterpret_cast<decltype(f.p)>(x);
     f.stride = x_stride;
-    f.vec = vec;
+    f.whole = whole;
     for (int64_t base = (int64_t)blockIdx.x * 256; base < total; base += step) {
         const int64_t at = base + threadIdx.x;
         if (at >= total) break;                                            // whole groups of four lanes leave together
         const int64_t row = at / units;
         const int unit = (int)(at - row * units);
-        const typename Factor::Raw raw = Factor::load(f, row, 8 * unit, dim - 8 * unit);
         f32x8 v;
-        if constexpr (DT == kTypeF32) v = raw.v;
-        else if constexpr (DT == kTypeF16) v = __builtin_convertvector(__builtin_bit_cast(h8, raw.v), f32x8);
-        else v = __builtin_convertvector(__builtin_bit_cast(bf8, raw.v), f32x8);
+        if (whole && 8 * unit < dim) {
+            v = eight(reinterpret_cast<const typename TypeOf<DT>::Element*>(x) + row * x_stride + 8 * unit);
+        } else {
+            const typename Factor::Raw raw = Factor::load(f, row, 8 * unit, dim - 8 * unit);
+            if constexpr (DT == kTypeF32) v = raw.v;
+            else if constexpr (DT == kTypeF16) v = __builtin_convertvector(__builtin_bit_cast(h8, raw.v), f32x8);
+            else v = __builtin_convertvector(__builtin_bit_cast(bf8, raw.v), f32x8);
+        }
         // magnitudes as bit patterns: their order is the numbers', infinities and NaN on top
         uint32_t top = 0;
 #pragma unroll
@@ -327,7 +430,7 @@ int launch_rows(RowsArgs a, hipStream_t st) {
 
 // The wide form wants 16-byte rows, a contraction of whole lines, and enough 256 x 256 tiles to be worth its size.
 bool wide_rows_fit(int dtype, const RowsArgs& a) {
-    return dtype != kTypeF32 && a.x_vec && a.w_vec && a.steps % 64 == 0 && a.cols >= 256 && a.x_stride < (1 << 21) &&
+    return dtype != kTypeF32 && a.x_whole && rows_aligned(dtype, a.w_stride) && a.steps % 64 == 0 && a.cols >= 256 &&
            a.groups.n >= 128 * (a.groups.offsets && !a.groups.whole ? (int64_t)a.groups.groups : 2);
 }
 
@@ -344,15 +447,13 @@ int launch_rows(int dtype, const RowsArgs& a, hipStream_t st) {
     return launch_rows<kTypeBF16, BACKWARD, false>(a, st);
 }
 
-template <bool TO_U, bool DOWN, bool SPLIT>
 int launch_few(int dtype, FewArgs a, hipStream_t st) {
     a.col_tiles = (a.cols + 15) / 16;
-    const int64_t blocks = row_tiles(a.groups, SPLIT ? 16 : 64) * a.col_tiles;
+    const int64_t blocks = row_tiles(a.groups, 16) * a.col_tiles;
     NEUS2_TRY(check_grid(blocks));
-    const dim3 grid((unsigned)blocks);
-    if (dtype == kTypeF32) few_rows_kernel<kTypeF32, TO_U, DOWN, SPLIT><<<grid, 256, 0, st>>>(a);
-    else if (dtype == kTypeF16) few_rows_kernel<kTypeF16, TO_U, DOWN, SPLIT><<<grid, 256, 0, st>>>(a);
-    else few_rows_kernel<kTypeBF16, TO_U, DOWN, SPLIT><<<grid, 256, 0, st>>>(a);
+    if (dtype == kTypeF32) few_rows_kernel<kTypeF32><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
+    else if (dtype == kTypeF16) few_rows_kernel<kTypeF16><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
+    else few_rows_kernel<kTypeBF16><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
     return check_launch("layer, few rows");
 }
 
@@ -365,27 +466,39 @@ RowGroups make_groups(const int32_t* offsets, int groups, int64_t n, bool whole)
     return g;
 }
 
-// u = scale A[slot] x (DOWN = false: matrices [slots][rank][steps]) or v = scale B[slot]^T dy (DOWN = true: [slots][steps][rank])
+template <int DT, bool DOWN>
+int launch_low_rank(const LowRankArgs& a, hipStream_t st) {
+    // contractions of up to 256 steps are not worth sharing: every wave has rows of its own
+    const bool split = a.steps > 256;
+    const int64_t blocks = row_tiles(a.groups, split ? 32 : 256);
+    NEUS2_TRY(check_grid(blocks));
+    const unsigned grid = (unsigned)blocks;
+    if (a.rank > 32) split ? low_rank_kernel<DT, DOWN, true, 2><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 2><<<grid, 512, 0, st>>>(a);
+    else split ? low_rank_kernel<DT, DOWN, true, 1><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 1><<<grid, 512, 0, st>>>(a);
+    return check_launch("adapter");
+}
+
+// u from x and A [slots][rank][steps], or v from dy and B [slots][steps][rank] (DOWN)
 template <bool DOWN>
 int launch_low_rank(const neus2_layer* l, const void* x, int64_t x_stride, const void* bank, const float* scales, const int32_t* slots,
                     const int32_t* offsets, int64_t n, int steps, float* u, hipStream_t st) {
-    FewArgs a = {};
+    LowRankArgs a = {};
     a.groups = make_groups(offsets, l->groups, n, false);
     a.x = x;
     a.x_stride = x_stride;
-    a.x_vec = rows_aligned(l->dtype, x_stride);
-    a.w = bank;
-    a.w_group = (int64_t)l->rank * steps;
-    a.w_stride = DOWN ? l->rank : steps;
-    a.w_vec = rows_aligned(l->dtype, steps);
+    a.x_whole = rows_whole(l->dtype, x_stride, steps);
+    a.bank = bank;
+    a.bank_slot = (int64_t)l->rank * steps;
+    a.bank_whole = rows_whole(l->dtype, steps, steps);
     a.steps = steps;
-    a.cols = l->rank;
-    a.y = u;
-    a.y_stride = l->rank;
+    a.rank = l->rank;
     a.slots = slots;
     a.n_slots = l->adapters;
     a.scales = scales;
-    return steps > 256 ? launch_few<true, DOWN, true>(l->dtype, a, st) : launch_few<true, DOWN, false>(l->dtype, a, st);
+    a.u = u;
+    if (l->dtype == kTypeF32) return launch_low_rank<kTypeF32, DOWN>(a, st);
+    if (l->dtype == kTypeF16) return launch_low_rank<kTypeF16, DOWN>(a, st);
+    return launch_low_rank<kTypeBF16, DOWN>(a, st);
 }
 
 // ---- argument checks ------------------------------------------------------------------------------------------------------------------
@@ -442,18 +555,18 @@ int neus2_grouped_fwd(const neus2_layer* l, const void* x, const void* W, const 
     if (n <= 16 * (int64_t)l->groups) {                       // 16 rows a group and fewer: the matrices are read once, and little else
         FewArgs a = {};
         a.groups = groups;
-        a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
-        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
         a.steps = l->in_dim; a.cols = l->out_dim;
+        a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
         a.y = y; a.y_stride = y_stride_of(l);
         a.relu = l->relu;
-        return launch_few<false, false, true>(l->dtype, a, st);
+        return launch_few(l->dtype, a, st);
     }
     RowsArgs a = {};
     a.groups = groups;
-    a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
-    a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
     a.steps = l->in_dim; a.cols = l->out_dim;
+        a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+    a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
     a.y = y; a.y_stride = y_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
     a.relu = l->relu;
     return launch_rows<false>(l->dtype, a, st);
@@ -489,9 +602,9 @@ int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
     if (dx && n > 0) {
         RowsArgs a = {};
         a.groups = make_groups(offsets, l->groups, n, false);
-        a.x = dy; a.x_stride = y_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
-        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
         a.steps = l->out_dim; a.cols = l->in_dim;
+        a.x = dy; a.x_stride = y_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
         a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
         a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
         NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
@@ -528,20 +641,20 @@ int neus2_adapter_fwd(const neus2_layer* l, const void* x, const void* W, const 
     if (n <= 64) {
         FewArgs a = {};
         a.groups = whole;
-        a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
-        a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
         a.steps = l->in_dim; a.cols = l->out_dim;
+        a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+        a.w = W; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
         a.y = y; a.y_stride = y_stride_of(l);
         a.relu = l->relu;
         a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
         a.u = u; a.bank = B; a.rank = l->rank;
-        return launch_few<false, false, true>(l->dtype, a, st);
+        return launch_few(l->dtype, a, st);
     }
     RowsArgs a = {};
     a.groups = whole;
-    a.x = x; a.x_stride = x_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
-    a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
     a.steps = l->in_dim; a.cols = l->out_dim;
+        a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+    a.w = W; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
     a.y = y; a.y_stride = y_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
     a.relu = l->relu;
     a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
@@ -594,9 +707,9 @@ int neus2_adapter_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
     if (dx && n > 0) {
         RowsArgs a = {};
         a.groups = make_groups(offsets, l->groups, n, true);
-        a.x = dy; a.x_stride = y_stride_of(l); a.x_vec = rows_aligned(l->dtype, a.x_stride);
-        a.w = W; a.w_stride = l->in_dim; a.w_vec = rows_aligned(l->dtype, l->in_dim);
         a.steps = l->out_dim; a.cols = l->in_dim;
+        a.x = dy; a.x_stride = y_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+        a.w = W; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
         a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
         a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
         a.segments = offsets; a.n_segments = l->groups; a.slots = slots; a.n_slots = l->adapters;
@@ -642,10 +755,10 @@ int neus2_pack8(int32_t dtype, const void* x, int64_t x_stride, int64_t n, int32
     hipStream_t st = (hipStream_t)stream;
     const int64_t stride = x_stride ? x_stride : dim, blocks = (n * ((dim + 31) / 32 * 4) + 255) / 256;
     const unsigned grid = (unsigned)(blocks < 8 * compute_units() ? blocks : 8 * compute_units());
-    const int vec = rows_aligned(dtype, stride);
-    if (dtype == kTypeF32) pack_kernel<kTypeF32><<<grid, 256, 0, st>>>(x, stride, vec, n, dim, q, e, masks);
-    else if (dtype == kTypeF16) pack_kernel<kTypeF16><<<grid, 256, 0, st>>>(x, stride, vec, n, dim, q, e, masks);
-    else pack_kernel<kTypeBF16><<<grid, 256, 0, st>>>(x, stride, vec, n, dim, q, e, masks);
+    const int whole = rows_aligned(dtype, stride) && dim % 8 == 0;
+    if (dtype == kTypeF32) pack_kernel<kTypeF32><<<grid, 256, 0, st>>>(x, stride, whole, n, dim, q, e, masks);
+    else if (dtype == kTypeF16) pack_kernel<kTypeF16><<<grid, 256, 0, st>>>(x, stride, whole, n, dim, q, e, masks);
+    else pack_kernel<kTypeBF16><<<grid, 256, 0, st>>>(x, stride, whole, n, dim, q, e, masks);
     return check_launch("pack8");
 }
 

@@ -10,12 +10,12 @@ namespace neus2 {
 namespace {
 
 template <class Factor>
-__device__ __forceinline__ typename Factor::Pointer make_pointer(const void* p, const uint8_t* e, int64_t stride, int vec) {
+__device__ __forceinline__ typename Factor::Pointer make_pointer(const void* p, const uint8_t* e, int64_t stride, int whole) {
     typename Factor::Pointer f;
     f.p = reinterpret_cast<decltype(f.p)>(p);
     f.stride = stride;
+    f.whole = whole;
     if constexpr (std::is_same_v<Factor, Packed<false>> || std::is_same_v<Factor, Packed<true>>) f.e = e;
-    else f.vec = vec;
     return f;
 }
 
@@ -36,8 +36,8 @@ __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
     const RowTile t = locate<true>(a.groups, a.chunk, 1, (int)(blockIdx.x / tiles), lane);
     if (t.group < 0) return;
 
-    const typename Left::Pointer left = make_pointer<Left>(a.left, nullptr, a.left_stride, a.left_vec);
-    const typename Right::Pointer right = make_pointer<Right>(a.right, a.right_e, a.right_stride, a.right_vec);
+    const typename Left::Pointer left = make_pointer<Left>(a.left, nullptr, a.left_stride, a.left_whole);
+    const typename Right::Pointer right = make_pointer<Right>(a.right, a.right_e, a.right_stride, a.right_whole);
     LeftTile lt;
     RightTile rt;
     v16f acc[kBO][kBI];
@@ -246,19 +246,20 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     a.partials = (int)partial_count(count, m.groups.n, splits, m.by_slot);
     a.by_slot = m.by_slot ? 1 : 0;
     if (m.left) {
-        a.left = m.left; a.left_stride = m.outer; a.left_vec = m.outer % 4 == 0;
+        a.left = m.left; a.left_stride = m.outer; a.left_whole = rows_whole(kTypeF32, m.outer, m.outer);
     } else {
-        a.left = m.dy; a.left_stride = m.dy_stride; a.left_vec = rows_aligned(m.dtype, m.dy_stride);
+        a.left = m.dy; a.left_stride = m.dy_stride; a.left_whole = rows_whole(m.dtype, m.dy_stride, m.outer);
     }
     if (m.right) {
-        a.right = m.right; a.right_stride = m.inner; a.right_vec = m.inner % 4 == 0;
+        a.right = m.right; a.right_stride = m.inner; a.right_whole = rows_whole(kTypeF32, m.inner, m.inner);
     } else if (m.xq) {
-        a.right = m.xq; a.right_e = m.xe; a.right_stride = (m.inner + 31) / 32 * 32;
+        a.right = m.xq; a.right_e = m.xe; a.right_stride = (m.inner + 31) / 32 * 32; a.right_whole = 1;
     } else {
-        a.right = m.x; a.right_stride = m.x_stride; a.right_vec = rows_aligned(m.dtype, m.x_stride);
+        a.right = m.x; a.right_stride = m.x_stride; a.right_whole = rows_whole(m.dtype, m.x_stride, m.inner);
     }
     const bool f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
-    const bool aligned = a.left_vec && (m.xq || a.right_vec) && m.dy_stride < (1 << 21) && m.x_stride < (1 << 21);
+    const bool aligned = rows_aligned(m.dtype, m.dy_stride) && m.dy_stride <= (1 << 20) &&
+                         (m.xq || (rows_aligned(m.dtype, m.x_stride) && m.x_stride <= (1 << 20)));
     const int to = wide && aligned ? kWideOuter : tile_of(m.outer), ti = wide && aligned ? kWideInner : tile_of(m.inner);
     a.outer_tiles = (a.outer + to - 1) / to;
     a.inner_tiles = (a.inner + ti - 1) / ti;
@@ -275,7 +276,7 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     } else if (f32) {
         m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
     } else if (wide && aligned) {
-        launch_wide_sums(m.dtype, m.xq != nullptr, a, blocks, st);
+        launch_wide_sums(m.dtype, m.xq != nullptr, a, grid, st);
     } else if (f16) {
         m.xq ? launch_sums<Native, Packed<true>, true>(a, grid, st) : launch_sums<Native, Native, true>(a, grid, st);
     } else {

@@ -27,8 +27,7 @@ struct WideTile {
     // from: where the tile begins; bytes: how far memory may be read from there on.  What lies beyond comes back as zero, except that
     // the last 16 bytes with something to read are read whole.
     __device__ __forceinline__ void load(const uint16_t* from, int64_t bytes, unsigned char* lds, int wave) const {
-        const int room = (int)(bytes < 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : (bytes + 15) & ~15);
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, room, 0x00020000);
+        const __amdgpu_buffer_rsrc_t r = make_window(from, bytes > 0x7ffffff0 ? bytes : (bytes + 15) & ~15);
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (wave + kWaves * q) * 1024), 16, (int)offset[q], 0, 0, 0);
@@ -201,49 +200,31 @@ __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wo = wave >> 2, wi = wave & 3;
     const int tiles = a.outer_tiles * a.inner_tiles;
-    Pieces pieces(count_tiles(a.groups, a.chunk, 1, lane) * tiles);
-    int outer0, inner0;
-    RowTile t;
-    auto place = [&](int piece, int& outer, int& inner, RowTile& chunk) {
-        const int tile = piece % tiles;
-        outer = tile / a.inner_tiles * kLeft;
-        inner = tile % a.inner_tiles * kRight;
-        chunk = locate<true>(a.groups, a.chunk, 1, piece / tiles, lane);
-    };
-    const int first = pieces.take();
-    if (first < 0) return;
-    place(first, outer0, inner0, t);
+    const int tile = (int)(blockIdx.x % tiles), outer0 = tile / a.inner_tiles * kLeft, inner0 = tile % a.inner_tiles * kRight;
+    const RowTile t = locate<true>(a.groups, a.chunk, 1, (int)(blockIdx.x / tiles), lane);
+    if (t.group < 0) return;
 
     WideTile<false, kLeft> lt;
     WideTile<false, kRight> rt;
     lt.begin(a.left_stride, wave, lane);
     rt.begin(a.right_stride, wave, lane);
-    int rows, inner_now, outer_now, hi, col8;
-    int64_t row8;
-    const uint16_t *left, *right;
+    int rows = t.hi - t.lo;
+    const int rounds = (rows + kDepth - 1) / kDepth, col8 = inner0 + 32 * (tid & 7);
+    const uint16_t* left = reinterpret_cast<const uint16_t*>(a.left) + (int64_t)t.lo * a.left_stride + outer0;
+    const uint16_t* right = reinterpret_cast<const uint16_t*>(a.right) + (PACKED ? 0 : (int64_t)t.lo * a.right_stride + inner0);
     typename Factor8::Pointer packed;
     packed.p = reinterpret_cast<const int8_t*>(a.right);
     packed.e = a.right_e;
     packed.stride = a.right_stride;
     typename Factor8::Raw raw[4];
-    auto begin = [&]() {
-        rows = t.hi - t.lo;
-        hi = t.hi;
-        outer_now = a.outer - outer0;
-        inner_now = a.inner - inner0;
-        left = reinterpret_cast<const uint16_t*>(a.left) + (int64_t)t.lo * a.left_stride + outer0;
-        right = reinterpret_cast<const uint16_t*>(a.right) + (PACKED ? 0 : (int64_t)t.lo * a.right_stride + inner0);
-        row8 = t.lo + (tid >> 3);
-        col8 = inner0 + 32 * (tid & 7);
-    };
     auto fetch = [&](unsigned char* l, unsigned char* r, bool more) {
-        lt.load(left, more ? ((int64_t)(rows - 1) * a.left_stride + outer_now) * 2 : 0, l, wave);
+        lt.load(left, more ? ((int64_t)(rows - 1) * a.left_stride + a.outer - outer0) * 2 : 0, l, wave);
         if (PACKED) {
+            const typename Factor8::Window w = Factor8::window(packed, t.hi - rows, inner0, more ? min(rows, kDepth) : 0, 0);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) raw[q] = Factor8::load(packed, row8, col8 + 8 * q, more && row8 < hi ? a.inner - (col8 + 8 * q) : 0);
-            row8 += kDepth;
+            for (int q = 0; q < 4; ++q) raw[q] = Factor8::fetch(w, tid >> 3, 32 * (tid & 7) + 8 * q, more && (tid >> 3) < rows && col8 < a.inner);
         } else {
-            rt.load(right, more ? ((int64_t)(rows - 1) * a.right_stride + inner_now) * 2 : 0, r, wave);
+            rt.load(right, more ? ((int64_t)(rows - 1) * a.right_stride + a.inner - inner0) * 2 : 0, r, wave);
             right += (int64_t)kDepth * a.right_stride;
         }
         left += (int64_t)kDepth * a.left_stride;
@@ -259,27 +240,15 @@ __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
             *reinterpret_cast<u32x4*>(r + line * (kRight * 2) + (((4 * (tid & 7) + q) ^ RightTile::across(line)) << 4)) = v[0];
         }
     };
-    begin();
-    fetch(left0, right0, rows > 0);
+    v16f acc[4][2];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
+    fetch(left0, right0, rounds > 0);
     loaded();
-    for (;;) {
-        v16f acc[4][2];
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) acc[c][r] = zero16();
-        const RowTile now = t;
-        const int now_outer = outer0, now_inner = inner0, rounds = (now.hi - now.lo + kDepth - 1) / kDepth, next = pieces.take();
-        if (next >= 0) place(next, outer0, inner0, t);
-        contract<kHalf, LeftTile, RightTile>(rounds, fetch, land, stages, wo, wi, lane, acc);
-        if (next >= 0) {
-            begin();
-            fetch(left0, right0, rows > 0);
-            loaded();
-        }
-        store_sums<4, 2>(a, now, now_outer + 128 * wo, now_inner + 64 * wi, acc, lane);
-        if (next < 0) break;
-    }
+    contract<kHalf, LeftTile, RightTile>(rounds, fetch, land, stages, wo, wi, lane, acc);
+    store_sums<4, 2>(a, t, outer0 + 128 * wo, inner0 + 64 * wi, acc, lane);
 }
 
 // one workgroup a compute unit, as many on every XCD
@@ -290,8 +259,7 @@ unsigned wide_blocks(int64_t pieces) {
 
 }  // namespace
 
-void launch_wide_sums(int dtype, bool packed, const SumArgs& a, int64_t pieces, hipStream_t st) {
-    const unsigned grid = wide_blocks(pieces);
+void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st) {
     if (dtype == kTypeF16) {
         if (packed) wide_sums_kernel<kTypeF16, true><<<grid, kThreads, 0, st>>>(a);
         else wide_sums_kernel<kTypeF16, false><<<grid, kThreads, 0, st>>>(a);

@@ -170,6 +170,10 @@ def test_the_binding_names_the_wrong_tensor():
         nb.pack8(x, torch.zeros(8, 32, dtype=torch.int8), torch.zeros(8, 2, dtype=torch.uint8))
     with pytest.raises(ValueError):
         nb.make_layer("f64", 1, 4, 4)
+    with pytest.raises(ValueError, match="host memory"):
+        nb.grouped_fwd(l, x, W, off, y)
+    with pytest.raises(ValueError, match="host memory"):
+        nb.pack8(x, torch.zeros(8, 32, dtype=torch.int8), torch.zeros(8, 1, dtype=torch.uint8))
 
 
 # ---- the oracle itself ---------------------------------------------------------------------------------------------------------
