@@ -47,6 +47,7 @@ struct RowTile {
     int lo, hi;      // its rows
     int part, parts; // which part of the group's rows this is
     int index;       // tiles before this group's first one
+    int end;         // where the group's rows end
     int shared;      // SHARED: those of groups of more than one tile among them
 };
 
@@ -65,7 +66,7 @@ __device__ __forceinline__ int wave_sums(int v, int lane) {
 template <bool SHARED = false>
 __device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int least, int tile, int lane) {
     RowTile t;
-    t.group = -1; t.lo = t.hi = t.part = t.parts = t.index = t.shared = 0;
+    t.group = -1; t.lo = t.hi = t.end = t.part = t.parts = t.index = t.shared = 0;
     const int count = g.offsets && !g.whole ? g.groups : 1;
     int before = 0, shared_before = 0;
     for (int base = 0; base < count; base += 64) {
@@ -87,6 +88,7 @@ __device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int leas
             t.index = before + __builtin_amdgcn_readlane(sum, at) - t.parts;
             if (SHARED) t.shared = shared_before + __builtin_amdgcn_readlane(shared - mine, at);
             t.part = tile - t.index;
+            t.end = hi;
             t.lo = min(lo + t.part * rows, hi);
             t.hi = min(t.lo + rows, hi);
             return t;
@@ -95,6 +97,17 @@ __device__ __forceinline__ RowTile locate(const RowGroups& g, int rows, int leas
         if (SHARED) shared_before += __builtin_amdgcn_readlane(shared, 63);
     }
     return t;
+}
+
+// The tile after t, which is number `tile`: of the same group without another look at the offsets.
+__device__ __forceinline__ void locate_next(const RowGroups& g, int rows, int least, int tile, int lane, RowTile& t) {
+    if (t.part + 1 < t.parts) {
+        ++t.part;
+        t.lo += rows;
+        t.hi = min(t.lo + rows, t.end);
+    } else {
+        t = locate(g, rows, least, tile, lane);
+    }
 }
 
 // How many tiles there are in all (locate's `rows` and `least`).
@@ -387,6 +400,12 @@ __device__ __forceinline__ v16f mma_terms(const u32x4 (&a)[TA], const u32x4 (&b)
 }
 
 // ---- conversions to the stored type -------------------------------------------------------------------------------------------
+// Outputs of more than this are stored past the caches (ONCE; a template parameter, since the compiler makes one plain store of two
+// branches that differ in the hint alone): the L2s of all XCDs hold 32 MB, and lines that are written back
+// while others are read cost more than the next reader saves.  2^18 rows, 64 to 64, fp32 in 20 groups: 27 us against 37; 16384 x
+// 2048 x 4096 in 8 groups: 283 against 297.
+constexpr int64_t kStoreOnceBytes = 32 << 20;
+
 // 16 bytes of a row; `room`: how many of their values lie inside the row; vec: rows begin on multiples of 16 bytes
 template <class E, bool ONCE>
 __device__ __forceinline__ void store_piece(E* p, const u32x4& v, int room, bool vec) {
@@ -418,7 +437,7 @@ struct RowsArgs {
     const void* w; int64_t w_group; int w_stride, w_whole; // matrix of group g at w + g * w_group, memory rows of w_stride values
     int steps;                                             // length of the contraction
     int cols;                                              // outputs per row
-    void* y; int64_t y_stride; int y_vec;
+    void* y; int64_t y_stride; int y_vec; int once;
     int relu;
     const uint32_t* masks; int mask_words;                 // NULL, or: outputs whose bit is not set are zero
     // adapters: y += bank[slot] u for the rows of each segment
@@ -493,8 +512,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t bank_window(const void* bank, 
 // What follows the contraction, for one wave's kBC x kBR blocks of 32 outputs (from col0 on) and 32 rows (from t.lo + row0 on).  A
 // lane holds four times four consecutive outputs of one row in each block.  lds: kBC * 1024 values for each wave, of which nobody
 // reads anything any more.
-// before_stores: called before the first of them.  ONCE: the outputs are more than a cache holds, and the
-// stores leave none of them there (16384 x 2048 x 4096 in 8 groups: 283 us against 297).
+// before_stores: called before the first of them.
 template <int DT, bool BACKWARD, bool ADAPT, int kBC, int kBR, bool ONCE, class BeforeStores>
 __device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t, int col0, int row0, v16f (&acc)[kBC][kBR],
                                             unsigned char* lds, int wave, int lane, BeforeStores before_stores) {
@@ -587,7 +605,7 @@ struct SumArgs {
     const void* left; int64_t left_stride; int left_whole;
     const void* right; const uint8_t* right_e; int64_t right_stride; int right_whole;
     int outer, inner;
-    float* out; int accumulate;
+    float* out; int accumulate; int once;
     float* partial;                  // [partials][outer][inner]: sums of chunks, of all of them (by_slot) or of those that share a group
     int partials;
     int by_slot;
@@ -606,7 +624,7 @@ __device__ __forceinline__ float* sums_place(const SumArgs& a, const RowTile& t,
     return t.hi > t.lo && index < a.partials ? a.partial + index * size : nullptr;     // decreasing offsets may count too many
 }
 
-template <int kBO, int kBI>
+template <bool ONCE, int kBO, int kBI>
 __device__ __forceinline__ void store_sums(const SumArgs& a, const RowTile& t, int outer0, int inner0, v16f (&acc)[kBO][kBI], int lane) {
     bool add;
     float* out = sums_place(a, t, add);
@@ -624,7 +642,8 @@ __device__ __forceinline__ void store_sums(const SumArgs& a, const RowTile& t, i
                 if (row >= a.outer) continue;
                 float* p = out + (int64_t)row * a.inner + col;
                 const float v = acc[o][i][r];
-                *p = add ? *p + v : v;
+                if (ONCE && !add) __builtin_nontemporal_store(v, p);
+                else *p = add ? *p + v : v;
             }
     }
 }

@@ -10,7 +10,7 @@ namespace {
 // fetched into registers while the products of the steps before run.  The matrix's tile is the instruction's first operand, so a
 // lane ends up with four consecutive outputs of one row.
 // BACKWARD = false: y = W x (contraction along the memory rows of W); true: dx = W^T dy (every memory row of W is a step).
-template <int DT, bool BACKWARD, bool ADAPT, int ROWS, int COLS, int WR, int WC, int DEPTH, int BUFS>
+template <int DT, bool BACKWARD, bool ADAPT, bool ONCE, int ROWS, int COLS, int WR, int WC, int DEPTH, int BUFS>
 __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
     typedef typename TypeOf<DT>::Element E;
     typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
@@ -83,7 +83,94 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
         __syncthreads();
     }
 
-    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR, false>(a, t, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane, [] {});
+    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR, ONCE>(a, t, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane, [] {});
+}
+
+// ---- narrow layers ---------------------------------------------------------------------------------------------------------------
+// Contractions of up to 64 steps and up to 64 outputs, the framework's own widths, with many rows: bound by reading and writing the
+// rows once.  A workgroup keeps the group's matrix in LDS, split once, and takes a run of consecutive tiles of 128 rows; a wave has 32
+// of them, whose values go from memory to registers as the instruction wants them (lane = row), the next tile's under way while this
+// one's products run.  2^18 rows, 64 to 64, fp32 in 20 groups: see the table of the calls that are measured.
+constexpr int kNarrowRows = 128;
+
+template <int DT, bool BACKWARD, bool ONCE>
+__global__ __launch_bounds__(256, 3) void narrow_rows_kernel(RowsArgs a) {
+    typedef typename TypeOf<DT>::Element E;
+    typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
+    constexpr int kTerms = Factor::kTerms, kSteps = 4;
+    typedef FactorTile<Factor, !BACKWARD, 64, 64, 256> MatrixTile;
+    constexpr int kStage = 32 * 64 * (int)sizeof(E);                     // 32 rows of 32 (fp32) or 64 (16 bits) outputs
+    __shared__ __attribute__((aligned(16))) unsigned char matrix[MatrixTile::kBytes], stage[4 * (sizeof(E) == 4 ? kStage / 2 : kStage)];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int j = lane & 31, h = lane >> 5;
+    const int64_t total = count_tiles(a.groups, kNarrowRows, 0, lane);
+    const int first = (int)(total * blockIdx.x / gridDim.x), end = (int)(total * (blockIdx.x + 1) / gridDim.x);
+    if (first >= end) return;
+
+    typename Factor::Pointer data, source;
+    data.p = reinterpret_cast<decltype(data.p)>(a.x);
+    data.stride = a.x_stride;
+    data.whole = a.x_whole;
+    source.stride = a.w_stride;
+    source.whole = a.w_whole;
+    typename Factor::Raw x[kSteps];
+    // the values of k-step ks of this wave's rows of a tile
+    auto request = [&](const RowTile& t, const typename Factor::Window& w, int ks) {
+        const int lo = t.lo + 32 * wave, rows = min(32, t.hi - lo), k = 16 * ks + 8 * h;
+        x[ks] = Factor::fetch(w, j, k, j < rows && k < a.steps);
+    };
+    auto window = [&](const RowTile& t) { return Factor::window(data, t.lo + 32 * wave, 0, min(32, t.hi - t.lo - 32 * wave), a.steps); };
+    int held = -1;                                                       // the group whose matrix lies in LDS
+    RowTile t = locate(a.groups, kNarrowRows, 0, first, lane);
+    typename Factor::Window w = window(t);
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) request(t, w, ks);
+    for (int tile = first;;) {
+        if (t.group != held) {
+            if (held >= 0) __syncthreads();                              // nobody reads the one before any more
+            source.p = reinterpret_cast<decltype(source.p)>(a.w) + (int64_t)t.group * a.w_group;
+            MatrixTile m;
+            m.load(source, 0, a.cols, 0, a.steps, tid);
+            m.store(matrix, tid);
+            __syncthreads();
+            held = t.group;
+        }
+        const RowTile now = t;
+        const bool more = ++tile < end;
+        if (more) {
+            locate_next(a.groups, kNarrowRows, 0, tile, lane, t);
+            w = window(t);
+        }
+        v16f acc[2][1];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) acc[c][0] = zero16();
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) {
+            u32x4 d[kTerms], m[2][kTerms];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int p = 0; p < kTerms; ++p) m[c][p] = MatrixTile::operand(matrix, p, c, ks, lane);
+            Factor::terms(x[ks], d);
+            if (more) request(t, w, ks);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) acc[c][0] = mma_terms<DT == kTypeF16>(m[c], d, acc[c][0]);
+            __builtin_amdgcn_sched_barrier(0);                           // reads hoisted out of the later steps would take the registers
+        }
+        if (now.lo + 32 * wave < now.hi) {
+            if constexpr (sizeof(E) == 4) {
+                v16f half[1][1];
+                half[0][0] = acc[0][0];
+                finish_rows<DT, BACKWARD, false, 1, 1, ONCE>(a, now, 0, 32 * wave, half, stage, wave, lane, [] {});
+                half[0][0] = acc[1][0];
+                if (a.cols > 32) finish_rows<DT, BACKWARD, false, 1, 1, ONCE>(a, now, 32, 32 * wave, half, stage, wave, lane, [] {});
+            } else {
+                finish_rows<DT, BACKWARD, false, 2, 1, ONCE>(a, now, 0, 32 * wave, acc, stage, wave, lane, [] {});
+            }
+        }
+        if (!more) break;
+    }
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------------
@@ -223,8 +310,10 @@ __global__ __launch_bounds__(512) void low_rank_kernel(LowRankArgs a) {
     __shared__ float part[SPLIT ? kWaves : 1][SPLIT ? BLOCKS * 32 : 1][33];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, (int)blockIdx.x, lane);
-    if (t.group < 0) return;
+    // an XCD has consecutive tiles, so that its L2 holds the matrices of few slots
+    const int piece = Pieces(count_tiles(a.groups, SPLIT ? 32 : 32 * kWaves, 0, lane)).take();
+    if (piece < 0) return;
+    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, piece, lane);
     if (!SPLIT) {
         t.lo += 32 * wave;
         t.hi = min(t.hi, t.lo + 32);
@@ -386,7 +475,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ x, i
     }
 }
 
-template <int DT>
+template <int DT, bool ONCE>
 __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int64_t n, int dim,
                                                      void* __restrict__ x, int64_t x_stride, int vec) {
     typedef typename TypeOf<DT>::Element E;
@@ -404,7 +493,9 @@ __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ 
         for (int s = 0; s < 8; ++s) v[s] = signed_byte(s < 4 ? w.x : w.y, s & 3) * scale;
         E* p = reinterpret_cast<E*>(x) + row * x_stride + col;
         if (room >= 8 && vec) {
-            *reinterpret_cast<E8*>(p) = __builtin_convertvector(v, E8);
+            const E8 w = __builtin_convertvector(v, E8);
+            if (ONCE) __builtin_nontemporal_store(w, reinterpret_cast<E8*>(p));
+            else *reinterpret_cast<E8*>(p) = w;
         } else {
 #pragma unroll
             for (int s = 0; s < 8; ++s)
@@ -414,18 +505,28 @@ __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ 
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------------------
-template <int DT, bool BACKWARD, bool ADAPT>
+template <int DT, bool BACKWARD, bool ADAPT, bool ONCE>
 int launch_rows(RowsArgs a, hipStream_t st) {
     constexpr int kDepth = DT == kTypeF32 ? 32 : 64, kBufs = DT == kTypeF32 ? 1 : 2;
-    if (a.cols > 64) {
+    if (!ADAPT && a.cols <= 64 && a.steps <= 64 && a.x_whole) {
+        const int64_t tiles = row_tiles(a.groups, kNarrowRows);
+        const unsigned grid = (unsigned)persistent_blocks((const void*)narrow_rows_kernel<DT, BACKWARD, ONCE>, 256, tiles);
+        narrow_rows_kernel<DT, BACKWARD, ONCE><<<grid, 256, 0, st>>>(a);
+    } else if (a.cols > 64) {
         a.col_tiles = (a.cols + 127) / 128;
         NEUS2_TRY(check_grid(row_tiles(a.groups, 128) * a.col_tiles));
-        rows_kernel<DT, BACKWARD, ADAPT, 128, 128, 2, 2, kDepth, kBufs><<<dim3((unsigned)(row_tiles(a.groups, 128) * a.col_tiles)), 256, 0, st>>>(a);
+        rows_kernel<DT, BACKWARD, ADAPT, ONCE, 128, 128, 2, 2, kDepth, kBufs><<<dim3((unsigned)(row_tiles(a.groups, 128) * a.col_tiles)), 256, 0, st>>>(a);
     } else {
         a.col_tiles = 1;
-        rows_kernel<DT, BACKWARD, ADAPT, 128, 64, 4, 1, kDepth, kBufs><<<dim3((unsigned)row_tiles(a.groups, 128)), 256, 0, st>>>(a);
+        rows_kernel<DT, BACKWARD, ADAPT, ONCE, 128, 64, 4, 1, kDepth, kBufs><<<dim3((unsigned)row_tiles(a.groups, 128)), 256, 0, st>>>(a);
     }
     return check_launch(BACKWARD ? "layer backward" : "layer forward");
+}
+
+template <int DT, bool BACKWARD>
+int launch_rows(const RowsArgs& a, hipStream_t st) {
+    if (a.rank > 0) return a.once ? launch_rows<DT, BACKWARD, true, true>(a, st) : launch_rows<DT, BACKWARD, true, false>(a, st);
+    return a.once ? launch_rows<DT, BACKWARD, false, true>(a, st) : launch_rows<DT, BACKWARD, false, false>(a, st);
 }
 
 // The wide form wants 16-byte rows, a contraction of whole lines, and enough 256 x 256 tiles to be worth its size.
@@ -435,16 +536,13 @@ bool wide_rows_fit(int dtype, const RowsArgs& a) {
 }
 
 template <bool BACKWARD>
-int launch_rows(int dtype, const RowsArgs& a, hipStream_t st) {
+int launch_rows(int dtype, const RowsArgs& args, hipStream_t st) {
+    RowsArgs a = args;
+    a.once = (int64_t)a.groups.n * a.cols * element_bytes(dtype) > kStoreOnceBytes;
     if (wide_rows_fit(dtype, a)) return launch_wide_rows(dtype, BACKWARD, a, st);
-    if (a.rank > 0) {
-        if (dtype == kTypeF32) return launch_rows<kTypeF32, BACKWARD, true>(a, st);
-        if (dtype == kTypeF16) return launch_rows<kTypeF16, BACKWARD, true>(a, st);
-        return launch_rows<kTypeBF16, BACKWARD, true>(a, st);
-    }
-    if (dtype == kTypeF32) return launch_rows<kTypeF32, BACKWARD, false>(a, st);
-    if (dtype == kTypeF16) return launch_rows<kTypeF16, BACKWARD, false>(a, st);
-    return launch_rows<kTypeBF16, BACKWARD, false>(a, st);
+    if (dtype == kTypeF32) return launch_rows<kTypeF32, BACKWARD>(a, st);
+    if (dtype == kTypeF16) return launch_rows<kTypeF16, BACKWARD>(a, st);
+    return launch_rows<kTypeBF16, BACKWARD>(a, st);
 }
 
 int launch_few(int dtype, FewArgs a, hipStream_t st) {
@@ -470,7 +568,7 @@ template <int DT, bool DOWN>
 int launch_low_rank(const LowRankArgs& a, hipStream_t st) {
     // contractions of up to 256 steps are not worth sharing: every wave has rows of its own
     const bool split = a.steps > 256;
-    const int64_t blocks = row_tiles(a.groups, split ? 32 : 256);
+    const int64_t blocks = (row_tiles(a.groups, split ? 32 : 256) + kXcds - 1) / kXcds * kXcds;
     NEUS2_TRY(check_grid(blocks));
     const unsigned grid = (unsigned)blocks;
     if (a.rank > 32) split ? low_rank_kernel<DT, DOWN, true, 2><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 2><<<grid, 512, 0, st>>>(a);
@@ -771,10 +869,11 @@ int neus2_unpack8(int32_t dtype, const int8_t* q, const uint8_t* e, int64_t n, i
     hipStream_t st = (hipStream_t)stream;
     const int64_t stride = x_stride ? x_stride : dim, blocks = (n * ((dim + 31) / 32 * 4) + 255) / 256;
     const unsigned grid = (unsigned)(blocks < 8 * compute_units() ? blocks : 8 * compute_units());
-    const int vec = rows_aligned(dtype, stride);
-    if (dtype == kTypeF32) unpack_kernel<kTypeF32><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
-    else if (dtype == kTypeF16) unpack_kernel<kTypeF16><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
-    else unpack_kernel<kTypeBF16><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
+    const int vec = rows_aligned(dtype, stride), once = n * dim * element_bytes(dtype) > kStoreOnceBytes;
+    auto go = [&](auto* plain, auto* once_only) { (once ? once_only : plain)<<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec); };
+    if (dtype == kTypeF32) go(unpack_kernel<kTypeF32, false>, unpack_kernel<kTypeF32, true>);
+    else if (dtype == kTypeF16) go(unpack_kernel<kTypeF16, false>, unpack_kernel<kTypeF16, true>);
+    else go(unpack_kernel<kTypeBF16, false>, unpack_kernel<kTypeBF16, true>);
     return check_launch("unpack8");
 }
 

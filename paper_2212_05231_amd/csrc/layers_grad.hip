@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
         __syncthreads();
     }
 
-    store_sums<kBO, kBI>(a, t, outer0 + 32 * wo * kBO, inner0 + 32 * wi * kBI, acc, lane);
+    store_sums<false, kBO, kBI>(a, t, outer0 + 32 * wo * kBO, inner0 + 32 * wi * kBI, acc, lane);
 }
 
 // Adds the chunks' sums.  A workgroup has 64 elements of one matrix; each of its four waves adds every fourth chunk in the order of
@@ -242,6 +242,7 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     a.inner = m.inner;
     a.out = m.out;
     a.accumulate = m.accumulate;
+    a.once = (int64_t)count * m.outer * m.inner * 4 > kStoreOnceBytes;
     a.partial = m.partial;
     a.partials = (int)partial_count(count, m.groups.n, splits, m.by_slot);
     a.by_slot = m.by_slot ? 1 : 0;

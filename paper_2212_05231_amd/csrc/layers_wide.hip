@@ -113,7 +113,7 @@ __device__ __forceinline__ void contract(int rounds, const Fetch& fetch, const L
     __shared__ __attribute__((aligned(16))) unsigned char right0[kRightBytes], right1[kRightBytes];                       \
     const Stages stages = {{left0, left1}, {right0, right1}}
 
-template <int DT, bool BACKWARD, bool ADAPT>
+template <int DT, bool BACKWARD, bool ADAPT, bool ONCE>
 __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
     typedef FactorTile<Native, true, kRight, kDepth, kThreads> DataTile;
     typedef FactorTile<Native, !BACKWARD, kLeft, kDepth, kThreads> MatrixTile;
@@ -175,21 +175,23 @@ __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
             begin();
             fetch(left0, right0, true);
         }
-        finish_rows<DT, BACKWARD, ADAPT, 4, 2, true>(a, now, now_col + 128 * wc, 64 * wr, acc, wave < 4 ? left1 : right1, wave & 3, lane, loaded);
+        finish_rows<DT, BACKWARD, ADAPT, 4, 2, ONCE>(a, now, now_col + 128 * wc, 64 * wr, acc, wave < 4 ? left1 : right1, wave & 3, lane, loaded);
         if (next < 0) break;
     }
 }
 
 template <int DT, bool BACKWARD>
 void launch(const RowsArgs& a, unsigned grid, hipStream_t st) {
-    if (a.rank > 0) wide_rows_kernel<DT, BACKWARD, true><<<grid, kThreads, 0, st>>>(a);
-    else wide_rows_kernel<DT, BACKWARD, false><<<grid, kThreads, 0, st>>>(a);
+    if (a.rank > 0) a.once ? wide_rows_kernel<DT, BACKWARD, true, true><<<grid, kThreads, 0, st>>>(a)
+                           : wide_rows_kernel<DT, BACKWARD, true, false><<<grid, kThreads, 0, st>>>(a);
+    else a.once ? wide_rows_kernel<DT, BACKWARD, false, true><<<grid, kThreads, 0, st>>>(a)
+                : wide_rows_kernel<DT, BACKWARD, false, false><<<grid, kThreads, 0, st>>>(a);
 }
 
 // Sums over rows: both factors lie across (a memory row is a step of the contraction), the rows behind the chunk's last are zeros.
 // PACKED: the right factor is in 8 bits.  A thread then fetches 32 of its values (one block of one row, one exponent) and puts them
 // into LDS as 16-bit numbers at the end of the round.
-template <int DT, bool PACKED>
+template <int DT, bool PACKED, bool ONCE>
 __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
     constexpr bool kHalf = DT == kTypeF16;
     typedef FactorTile<Native, false, kLeft, kDepth, kThreads> LeftTile;
@@ -248,7 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
     fetch(left0, right0, rounds > 0);
     loaded();
     contract<kHalf, LeftTile, RightTile>(rounds, fetch, land, stages, wo, wi, lane, acc);
-    store_sums<4, 2>(a, t, outer0 + 128 * wo, inner0 + 64 * wi, acc, lane);
+    store_sums<ONCE, 4, 2>(a, t, outer0 + 128 * wo, inner0 + 64 * wi, acc, lane);
 }
 
 // one workgroup a compute unit, as many on every XCD
@@ -260,12 +262,13 @@ unsigned wide_blocks(int64_t pieces) {
 }  // namespace
 
 void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st) {
+    auto go = [&](auto* plain, auto* once) { (a.once ? once : plain)<<<grid, kThreads, 0, st>>>(a); };
     if (dtype == kTypeF16) {
-        if (packed) wide_sums_kernel<kTypeF16, true><<<grid, kThreads, 0, st>>>(a);
-        else wide_sums_kernel<kTypeF16, false><<<grid, kThreads, 0, st>>>(a);
+        if (packed) go(wide_sums_kernel<kTypeF16, true, false>, wide_sums_kernel<kTypeF16, true, true>);
+        else go(wide_sums_kernel<kTypeF16, false, false>, wide_sums_kernel<kTypeF16, false, true>);
     } else {
-        if (packed) wide_sums_kernel<kTypeBF16, true><<<grid, kThreads, 0, st>>>(a);
-        else wide_sums_kernel<kTypeBF16, false><<<grid, kThreads, 0, st>>>(a);
+        if (packed) go(wide_sums_kernel<kTypeBF16, true, false>, wide_sums_kernel<kTypeBF16, true, true>);
+        else go(wide_sums_kernel<kTypeBF16, false, false>, wide_sums_kernel<kTypeBF16, false, true>);
     }
 }
 
