@@ -469,37 +469,46 @@ __device__ __forceinline__ f32x8 load_u(__amdgpu_buffer_rsrc_t u, int row, int r
     return v;
 }
 
-template <int DT>
-__device__ __forceinline__ float window_value(__amdgpu_buffer_rsrc_t w, uint32_t index, bool in) {
-    typedef typename TypeOf<DT>::Element E;
-    if constexpr (DT == kTypeF32) return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(w, (int)(in ? index * 4u : kOutside), 0, 0));
-    else return (float)__builtin_bit_cast(E, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(w, (int)(in ? index * 2u : kOutside), 0, 0));
+// eight values bank(col, k .. k + 7) of a window over one adapter's matrix, as they lie in memory: along the memory row forward (bank
+// [col][rank]), down the column backward ([rank][cols])
+template <int DT> struct BankRaw { u32x4 v[DT == kTypeF32 ? 2 : 1]; };
+
+template <int DT, bool BACKWARD>
+__device__ __forceinline__ BankRaw<DT> request_bank(__amdgpu_buffer_rsrc_t bank, int rank, int cols, int col, int k) {
+    constexpr uint32_t kBytes = DT == kTypeF32 ? 4 : 2;
+    BankRaw<DT> raw;
+    if (!BACKWARD && (rank & 7) == 0) {
+        const uint32_t at = (uint32_t)(col * rank + k) * kBytes;
+        const bool in = col < cols && k < rank;
+        raw.v[0] = window16(bank, in ? at : kOutside);
+        if constexpr (DT == kTypeF32) raw.v[1] = window16(bank, in ? at + 16u : kOutside);
+    } else {
+        uint32_t bits[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const uint32_t at = (uint32_t)(BACKWARD ? (k + s) * cols + col : col * rank + k + s) * kBytes;
+            const bool in = col < cols && k + s < rank;
+            if constexpr (DT == kTypeF32) bits[s] = __builtin_amdgcn_raw_buffer_load_b32(bank, (int)(in ? at : kOutside), 0, 0);
+            else bits[s] = __builtin_amdgcn_raw_buffer_load_b16(bank, (int)(in ? at : kOutside), 0, 0);
+        }
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            if constexpr (DT == kTypeF32) raw.v[s >> 2][s & 3] = bits[s];
+            else if (s % 2 == 0) raw.v[0][s >> 1] = bits[s] | bits[s + 1] << 16;
+        }
+    }
+    return raw;
 }
 
-// eight values bank(col, k .. k + 7) of a window over one adapter's matrix: along the memory row forward (bank [col][rank]), down the
-// column backward ([rank][cols])
-template <int DT, bool BACKWARD>
-__device__ __forceinline__ f32x8 load_bank(__amdgpu_buffer_rsrc_t bank, int rank, int cols, int col, int k) {
-    typedef typename TypeOf<DT>::Element E;
-    f32x8 v;
-    if (!BACKWARD && (rank & 7) == 0) {
-        const uint32_t at = (uint32_t)(col * rank + k) * (uint32_t)sizeof(E);
-        const bool in = col < cols && k < rank;
-        const u32x4 a = window16(bank, in ? at : kOutside);
-        if constexpr (DT == kTypeF32) {
-            const v4f b = __builtin_bit_cast(v4f, window16(bank, in ? at + 16u : kOutside));
-            v = __builtin_shufflevector(__builtin_bit_cast(v4f, a), b, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else if constexpr (DT == kTypeF16) {
-            v = __builtin_convertvector(__builtin_bit_cast(h8, a), f32x8);
-        } else {
-            v = __builtin_convertvector(__builtin_bit_cast(bf8, a), f32x8);
-        }
+template <int DT>
+__device__ __forceinline__ void bank_terms(const BankRaw<DT>& raw, u32x4 (&out)[AdapterTerms<DT>::kBank]) {
+    if constexpr (DT == kTypeF32) {
+        split8<3>(__builtin_shufflevector(__builtin_bit_cast(v4f, raw.v[0]), __builtin_bit_cast(v4f, raw.v[1]), 0, 1, 2, 3, 4, 5, 6, 7), out);
+    } else if constexpr (DT == kTypeF16) {
+        split8<2>(__builtin_convertvector(__builtin_bit_cast(h8, raw.v[0]), f32x8), out);
     } else {
-#pragma unroll
-        for (int s = 0; s < 8; ++s)
-            v[s] = window_value<DT>(bank, (uint32_t)(BACKWARD ? (k + s) * cols + col : col * rank + k + s), col < cols && k + s < rank);
+        out[0] = raw.v[0];
     }
-    return v;
 }
 
 template <int DT>
@@ -509,12 +518,31 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t bank_window(const void* bank, 
     return make_window(reinterpret_cast<const E*>(bank) + slot * size, size * (int64_t)sizeof(E));
 }
 
+// The segments from number `base` on, one a lane: fetched before the contraction, so that what follows it waits for none of this.
+struct Segments {
+    int base, lo, hi, slot;
+    __device__ __forceinline__ void fetch(const RowsArgs& a, int from, int lane) {
+        base = from;
+        const int s = from + lane;
+        lo = hi = 0x7fffffff;
+        slot = -1;
+        if (s < a.n_segments) {
+            lo = a.segments[s];
+            hi = a.segments[s + 1];
+            slot = slot_of(a.slots, a.n_slots, s);
+        }
+    }
+    __device__ __forceinline__ void begin(const RowsArgs& a, const RowTile& t, int lane) {
+        fetch(a, segment_of(a.segments, a.n_segments, t.lo, lane), lane);
+    }
+};
+
 // What follows the contraction, for one wave's kBC x kBR blocks of 32 outputs (from col0 on) and 32 rows (from t.lo + row0 on).  A
 // lane holds four times four consecutive outputs of one row in each block.  lds: kBC * 1024 values for each wave, of which nobody
 // reads anything any more.
 // before_stores: called before the first of them.
 template <int DT, bool BACKWARD, bool ADAPT, int kBC, int kBR, bool ONCE, class BeforeStores>
-__device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t, int col0, int row0, v16f (&acc)[kBC][kBR],
+__device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t, Segments segments, int col0, int row0, v16f (&acc)[kBC][kBR],
                                             unsigned char* lds, int wave, int lane, BeforeStores before_stores) {
     typedef typename TypeOf<DT>::Element E;
     const int j = lane & 31, h = lane >> 5;
@@ -523,14 +551,21 @@ __device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t,
         // other segments zero.  A tile inside one segment takes rank / 16 more k-steps.
         constexpr int kU = AdapterTerms<DT>::kU, kBank = AdapterTerms<DT>::kBank;
         const __amdgpu_buffer_rsrc_t us = make_window(a.u + (int64_t)t.lo * a.rank, (int64_t)(t.hi - t.lo) * a.rank * 4);
-        int s = segment_of(a.segments, a.n_segments, t.lo, lane);
-        for (; s < a.n_segments; ++s) {
-            const int lo = max(a.segments[s], t.lo), hi = min(a.segments[s + 1], t.hi);
+        for (int i = 0;; ++i) {
+            if (i == 64) {
+                segments.fetch(a, segments.base + 64, lane);
+                i = 0;
+            }
+            const int lo = max(__builtin_amdgcn_readlane(segments.lo, i), t.lo), hi = min(__builtin_amdgcn_readlane(segments.hi, i), t.hi);
             if (lo >= t.hi) break;
-            const int slot = hi > lo ? slot_of(a.slots, a.n_slots, s) : -1;
+            const int slot = hi > lo ? __builtin_amdgcn_readlane(segments.slot, i) : -1;
             if (slot < 0) continue;
             const __amdgpu_buffer_rsrc_t bank = bank_window<DT>(a.bank, slot, a.rank, a.cols);
             for (int k0 = 0; k0 < a.rank; k0 += 16) {
+                // the bank's operands are all requested before the first is used
+                BankRaw<DT> raw[kBC];
+#pragma unroll
+                for (int c = 0; c < kBC; ++c) raw[c] = request_bank<DT, BACKWARD>(bank, a.rank, a.cols, col0 + 32 * c + j, k0 + 8 * h);
                 u32x4 u[kBR][kU];
 #pragma unroll
                 for (int r = 0; r < kBR; ++r) {
@@ -540,7 +575,7 @@ __device__ __forceinline__ void finish_rows(const RowsArgs& a, const RowTile& t,
 #pragma unroll
                 for (int c = 0; c < kBC; ++c) {
                     u32x4 b[kBank];
-                    split8<kBank>(load_bank<DT, BACKWARD>(bank, a.rank, a.cols, col0 + 32 * c + j, k0 + 8 * h), b);
+                    bank_terms<DT>(raw[c], b);
 #pragma unroll
                     for (int r = 0; r < kBR; ++r) {
                         const int first = t.lo + row0 + 32 * r;

@@ -44,6 +44,8 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
 #pragma unroll
         for (int r = 0; r < kBR; ++r) acc[c][r] = zero16();
 
+    Segments segments = {};
+    if (ADAPT) segments.begin(a, t, lane);
     const int rounds = (a.steps + DEPTH - 1) / DEPTH;
     dt.load(data, t.lo, t.hi - t.lo, 0, a.steps, tid);
     mt.load(matrix, col0, a.cols - col0, 0, a.steps, tid);
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
         __syncthreads();
     }
 
-    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR, ONCE>(a, t, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane, [] {});
+    finish_rows<DT, BACKWARD, ADAPT, kBC, kBR, ONCE>(a, t, segments, col0 + 32 * wc * kBC, 32 * wr * kBR, acc, lds, wave, lane, [] {});
 }
 
 // ---- narrow layers ---------------------------------------------------------------------------------------------------------------
@@ -162,11 +164,11 @@ __global__ __launch_bounds__(256, 3) void narrow_rows_kernel(RowsArgs a) {
             if constexpr (sizeof(E) == 4) {
                 v16f half[1][1];
                 half[0][0] = acc[0][0];
-                finish_rows<DT, BACKWARD, false, 1, 1, ONCE>(a, now, 0, 32 * wave, half, stage, wave, lane, [] {});
+                finish_rows<DT, BACKWARD, false, 1, 1, ONCE>(a, now, {}, 0, 32 * wave, half, stage, wave, lane, [] {});
                 half[0][0] = acc[1][0];
-                if (a.cols > 32) finish_rows<DT, BACKWARD, false, 1, 1, ONCE>(a, now, 32, 32 * wave, half, stage, wave, lane, [] {});
+                if (a.cols > 32) finish_rows<DT, BACKWARD, false, 1, 1, ONCE>(a, now, {}, 32, 32 * wave, half, stage, wave, lane, [] {});
             } else {
-                finish_rows<DT, BACKWARD, false, 2, 1, ONCE>(a, now, 0, 32 * wave, acc, stage, wave, lane, [] {});
+                finish_rows<DT, BACKWARD, false, 2, 1, ONCE>(a, now, {}, 0, 32 * wave, acc, stage, wave, lane, [] {});
             }
         }
         if (!more) break;
@@ -223,6 +225,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewArgs a) {
     // A wave's part of the contraction is one piece: rows that lie a power of two apart hang on the same memory channels, and waves
     // that walk side by side would all be at the same few of them.
     const int length = (a.steps + kFewWaves * kChunk - 1) / (kFewWaves * kChunk) * kChunk, end = min(a.steps, (wave + 1) * length);
+    auto find_slots = [&] {                                               // the adapters of this wave's share of the rows
+        if (a.rank == 0) return;
+#pragma unroll
+        for (int r = 0; r < 16 / kFewWaves; ++r) {
+            const int of = 16 / kFewWaves * wave + r, s = segment_of(a.segments, a.n_segments, min(t.lo + of, t.hi - 1), lane);
+            const int slot = s < a.n_segments ? slot_of(a.slots, a.n_slots, s) : -1;
+            if (lane == 0) row_slot[of] = slot;
+        }
+    };
+    if (wave * length >= end) find_slots();
     for (int base = wave * length; base < end; base += kAhead * kChunk) {
         typename Factor::Raw w[kAhead][kUnits], x[kAhead][kUnits];
 #pragma unroll
@@ -238,6 +250,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewArgs a) {
                     x[q][v] = Factor::load(data, t.lo + i, k, row_in ? end - k : 0);
                 }
             }
+        if (base == wave * length) find_slots();                          // while the first loads are under way
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
 #pragma unroll
@@ -253,14 +266,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewArgs a) {
             }
     }
     // lane: row lane % 16, outputs 4 (lane / 16) .. + 3
-    if (a.rank > 0) {
-#pragma unroll
-        for (int r = 0; r < 16 / kFewWaves; ++r) {
-            const int of = 16 / kFewWaves * wave + r, s = segment_of(a.segments, a.n_segments, min(t.lo + of, t.hi - 1), lane);
-            const int slot = s < a.n_segments ? slot_of(a.slots, a.n_slots, s) : -1;
-            if (lane == 0) row_slot[of] = slot;
-        }
-    }
     part[wave][lane] = acc;
     __syncthreads();
     // a thread per output, the outputs of a row side by side
@@ -301,30 +306,30 @@ struct LowRankArgs {
 };
 
 template <int DT, bool DOWN, bool SPLIT, int BLOCKS>
-__global__ __launch_bounds__(512) void low_rank_kernel(LowRankArgs a) {
+__global__ __launch_bounds__(512, SPLIT ? 4 : 2) void low_rank_kernel(LowRankArgs a) {
     typedef typename TypeOf<DT>::Element E;
     typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
-    constexpr int kTerms = Factor::kTerms, kAhead = 4;        // k-steps whose operands are in flight together
+    constexpr int kTerms = Factor::kTerms;
+    // k-steps (of 32) whose operands are in flight together: as many as leave registers for a second workgroup on the compute unit
+    constexpr int kAhead = DT == kTypeF32 ? (BLOCKS > 2 ? 1 : 2) : BLOCKS > 2 ? (DOWN ? 1 : 2) : DOWN && BLOCKS > 1 ? 2 : 4;
     constexpr bool kHalf = DT == kTypeF16;
     constexpr int kWaves = 8;
-    __shared__ float part[SPLIT ? kWaves : 1][SPLIT ? BLOCKS * 32 : 1][33];
+    __shared__ float part[SPLIT ? kWaves : 1][SPLIT ? BLOCKS * 16 : 1][33];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // an XCD has consecutive tiles, so that its L2 holds the matrices of few slots
-    const int piece = Pieces(count_tiles(a.groups, SPLIT ? 32 : 32 * kWaves, 0, lane)).take();
-    if (piece < 0) return;
-    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, piece, lane);
+    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, (int)blockIdx.x, lane);
+    if (t.group < 0) return;
     if (!SPLIT) {
         t.lo += 32 * wave;
         t.hi = min(t.hi, t.lo + 32);
         if (t.lo >= t.hi) return;
     }
     const int slot = slot_of(a.slots, a.n_slots, t.group);
-    const int j = lane & 31, h = lane >> 5;
     if (slot < 0) {
         for (int i = SPLIT ? tid : lane; i < (t.hi - t.lo) * a.rank; i += SPLIT ? 512 : 64) a.u[(int64_t)t.lo * a.rank + i] = 0.f;
         return;
     }
+    const float scale = a.scales[slot];
     typename Factor::Pointer data, matrix;
     data.p = reinterpret_cast<decltype(data.p)>(a.x);
     data.stride = a.x_stride;
@@ -332,28 +337,34 @@ __global__ __launch_bounds__(512) void low_rank_kernel(LowRankArgs a) {
     matrix.p = reinterpret_cast<decltype(matrix.p)>(a.bank) + (int64_t)slot * a.bank_slot;
     matrix.stride = a.steps;
     matrix.whole = a.bank_whole;
-    const bool row_in = t.lo + j < t.hi;
     const typename Factor::Window xs = Factor::window(data, t.lo, 0, t.hi - t.lo, a.steps), bs = Factor::window(matrix, 0, 0, a.rank, a.steps);
     const __amdgpu_buffer_rsrc_t down = make_window(matrix.p, a.bank_slot * (int64_t)sizeof(E));
     const bool whole = a.x_whole && (DOWN || a.bank_whole);
-    v16f acc[BLOCKS];
+    const int i = lane & 15, quarter = lane >> 4, rows = t.hi - t.lo;
+    v4f acc[BLOCKS][2];
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) acc[b] = zero16();
-    constexpr int kRun = 16 * kAhead;
-    const int length = (a.steps + kWaves * kRun - 1) / (kWaves * kRun) * kRun;          // one piece for every wave, see above
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) acc[b][r] = v4f{0.f, 0.f, 0.f, 0.f};
+    constexpr int kRun = 32 * kAhead;
+    const int length = (a.steps + kWaves * 32 - 1) / (kWaves * 32) * 32;                // one piece for every wave, see above
     const int end = SPLIT ? min(a.steps, (wave + 1) * length) : a.steps;
     for (int base = SPLIT ? wave * length : 0; base < end; base += kRun) {
-        typename Factor::Raw x[kAhead], w[BLOCKS][kAhead];
+        typename Factor::Raw x[2][kAhead], w[BLOCKS][kAhead];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-            const int k = base + 16 * q + 8 * h;
-            if (whole) x[q] = Factor::fetch(xs, j, k, row_in && k < end);
-            else x[q] = Factor::load(data, t.lo + j, k, row_in ? end - k : 0);
+            const int k = base + 32 * q + 8 * quarter;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = 16 * r + i;
+                if (whole) x[r][q] = Factor::fetch(xs, row, k, row < rows && k < end);
+                else x[r][q] = Factor::load(data, t.lo + row, k, row < rows ? end - k : 0);
+            }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
-                const int r = 32 * b + j;
+                const int r = 16 * b + i;
                 if constexpr (DOWN) {
-                    // eight values below each other, of 32 columns side by side; their bits as they are
+                    // eight values below each other, of 16 columns side by side; their bits as they are
                     uint32_t bits[8];
 #pragma unroll
                     for (int s = 0; s < 8; ++s) {
@@ -376,40 +387,56 @@ __global__ __launch_bounds__(512) void low_rank_kernel(LowRankArgs a) {
         }
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-            u32x4 xt[kTerms], wt[kTerms];
-            Factor::terms(x[q], xt);
+            u32x4 xt[2][kTerms], wt[kTerms];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) Factor::terms(x[r][q], xt[r]);
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 Factor::terms(w[b][q], wt);
-                acc[b] = mma_terms<kHalf>(wt, xt, acc[b]);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int p = 0; p < kTerms; ++p)
+#pragma unroll
+                        for (int o = 0; o < kTerms; ++o)
+                            if (p + o < kTerms) acc[b][r] = mma16<kHalf>(wt[p], xt[r][o], acc[b][r]);
             }
         }
     }
-    // lane: row j, outputs 32 b + neuron_of(r, h)
-    const float scale = a.scales[slot];
+    // lane: row 16 r + lane % 16, outputs 16 b + 4 (lane / 16) .. + 3
     if constexpr (SPLIT) {
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) part[wave][32 * b + neuron_of(r, h)][j] = acc[b][r];
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) part[wave][16 * b + 4 * quarter + v][16 * r + i] = acc[b][r][v];
         __syncthreads();
-        for (int i = tid; i < 32 * a.rank; i += 512) {
-            const int row = i / a.rank, r = i - row * a.rank;
-            if (t.lo + row >= t.hi) break;
+        for (int at = tid; at < 32 * a.rank; at += 512) {
+            const int row = at / a.rank, r = at - row * a.rank;
+            if (row >= rows) break;
             float z = 0.f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) z += part[w][r][row];
-            a.u[(int64_t)t.lo * a.rank + i] = z * scale;
+            a.u[(int64_t)t.lo * a.rank + at] = z * scale;
         }
-    } else if (row_in) {
-        float* out = a.u + (int64_t)(t.lo + j) * a.rank;
+    } else {
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
+        for (int r = 0; r < 2; ++r) {
+            if (16 * r + i >= rows) continue;
+            float* out = a.u + (int64_t)(t.lo + 16 * r + i) * a.rank + 4 * quarter;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int at = 32 * b + neuron_of(r, h);
-                if (at < a.rank) out[at] = acc[b][r] * scale;
+            for (int b = 0; b < BLOCKS; ++b) {
+                const v4f z = acc[b][r] * scale;
+                if (a.rank % 4 == 0) {
+                    if (16 * b + 4 * quarter < a.rank) *reinterpret_cast<v4f*>(out + 16 * b) = z;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (16 * b + 4 * quarter + v < a.rank) out[16 * b + v] = z[v];
+                }
             }
+        }
     }
 }
 
@@ -475,7 +502,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* __restrict__ x, i
     }
 }
 
-template <int DT, bool ONCE>
+template <int DT>
 __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int64_t n, int dim,
                                                      void* __restrict__ x, int64_t x_stride, int vec) {
     typedef typename TypeOf<DT>::Element E;
@@ -493,9 +520,7 @@ __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ 
         for (int s = 0; s < 8; ++s) v[s] = signed_byte(s < 4 ? w.x : w.y, s & 3) * scale;
         E* p = reinterpret_cast<E*>(x) + row * x_stride + col;
         if (room >= 8 && vec) {
-            const E8 w = __builtin_convertvector(v, E8);
-            if (ONCE) __builtin_nontemporal_store(w, reinterpret_cast<E8*>(p));
-            else *reinterpret_cast<E8*>(p) = w;
+            *reinterpret_cast<E8*>(p) = __builtin_convertvector(v, E8);
         } else {
 #pragma unroll
             for (int s = 0; s < 8; ++s)
@@ -568,10 +593,11 @@ template <int DT, bool DOWN>
 int launch_low_rank(const LowRankArgs& a, hipStream_t st) {
     // contractions of up to 256 steps are not worth sharing: every wave has rows of its own
     const bool split = a.steps > 256;
-    const int64_t blocks = (row_tiles(a.groups, split ? 32 : 256) + kXcds - 1) / kXcds * kXcds;
+    const int64_t blocks = row_tiles(a.groups, split ? 32 : 256);
     NEUS2_TRY(check_grid(blocks));
     const unsigned grid = (unsigned)blocks;
-    if (a.rank > 32) split ? low_rank_kernel<DT, DOWN, true, 2><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 2><<<grid, 512, 0, st>>>(a);
+    if (a.rank > 32) split ? low_rank_kernel<DT, DOWN, true, 4><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 4><<<grid, 512, 0, st>>>(a);
+    else if (a.rank > 16) split ? low_rank_kernel<DT, DOWN, true, 2><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 2><<<grid, 512, 0, st>>>(a);
     else split ? low_rank_kernel<DT, DOWN, true, 1><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 1><<<grid, 512, 0, st>>>(a);
     return check_launch("adapter");
 }
@@ -869,11 +895,10 @@ int neus2_unpack8(int32_t dtype, const int8_t* q, const uint8_t* e, int64_t n, i
     hipStream_t st = (hipStream_t)stream;
     const int64_t stride = x_stride ? x_stride : dim, blocks = (n * ((dim + 31) / 32 * 4) + 255) / 256;
     const unsigned grid = (unsigned)(blocks < 8 * compute_units() ? blocks : 8 * compute_units());
-    const int vec = rows_aligned(dtype, stride), once = n * dim * element_bytes(dtype) > kStoreOnceBytes;
-    auto go = [&](auto* plain, auto* once_only) { (once ? once_only : plain)<<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec); };
-    if (dtype == kTypeF32) go(unpack_kernel<kTypeF32, false>, unpack_kernel<kTypeF32, true>);
-    else if (dtype == kTypeF16) go(unpack_kernel<kTypeF16, false>, unpack_kernel<kTypeF16, true>);
-    else go(unpack_kernel<kTypeBF16, false>, unpack_kernel<kTypeBF16, true>);
+    const int vec = rows_aligned(dtype, stride);
+    if (dtype == kTypeF32) unpack_kernel<kTypeF32><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
+    else if (dtype == kTypeF16) unpack_kernel<kTypeF16><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
+    else unpack_kernel<kTypeBF16><<<grid, 256, 0, st>>>(q, e, n, dim, x, stride, vec);
     return check_launch("unpack8");
 }
 

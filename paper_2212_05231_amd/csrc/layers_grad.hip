@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
     store_sums<false, kBO, kBI>(a, t, outer0 + 32 * wo * kBO, inner0 + 32 * wi * kBI, acc, lane);
 }
 
-// Adds the chunks' sums.  A workgroup has 64 elements of one matrix; each of its four waves adds every fourth chunk in the order of
+// Adds the chunks' sums.  A workgroup has 256 elements of one matrix; each of its four waves adds every fourth chunk in the order of
 // the rows, then the four sums are added, so the order is always the same.
 struct JoinArgs {
     RowGroups groups;
@@ -102,31 +102,38 @@ struct JoinArgs {
 };
 
 __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs a) {
-    __shared__ float sums[4][64];
+    __shared__ v4f sums[4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int matrix = (int)(blockIdx.x / a.blocks);
     const int groups = a.groups.offsets ? a.groups.groups : 1;
+    const bool fours = a.size % 4 == 0;
     int at0 = 0, parts0 = 0;                                                     // a group's parts, if there is only one group
     bool mine = a.by_slot != 0;
-    for (int64_t first = (int64_t)(blockIdx.x % a.blocks) * 64; first < a.size; first += (int64_t)a.blocks * 64) {
-        const int64_t at = first + lane;
-        const bool in = at < a.size;
-        float sum = 0.f;
+    for (int64_t first = (int64_t)(blockIdx.x % a.blocks) * 256; first < a.size; first += (int64_t)a.blocks * 256) {
+        const int64_t at = first + 4 * lane;
+        const int room = (int)min((int64_t)4, a.size - at);                      // of this lane's four elements, how many there are
+        v4f sum = {0.f, 0.f, 0.f, 0.f};
         int turn = 0;                                                            // chunks so far, modulo the waves
+        auto part = [&](int p) {
+            const float* src = a.partial + (int64_t)p * a.size + at;
+            if (fours) return room > 0 ? *reinterpret_cast<const v4f*>(src) : v4f{0.f, 0.f, 0.f, 0.f};
+            v4f v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = e < room ? src[e] : 0.f;
+            return v;
+        };
         auto add_parts = [&](int index, int parts) {
             const int end = min(index + parts, a.partials);                      // decreasing offsets may count too many
             int p = index + ((wave - turn) & 3);
             turn = (turn + parts) & 3;
-            if (!in) return;
-            const float* src = a.partial + at;
             for (; p + 12 < end; p += 16) {
-                float v[4];
+                v4f v[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = src[(int64_t)(p + 4 * q) * a.size];
+                for (int q = 0; q < 4; ++q) v[q] = part(p + 4 * q);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) sum += v[q];
             }
-            for (; p < end; p += 4) sum += src[(int64_t)p * a.size];
+            for (; p < end; p += 4) sum += part(p);
         };
         if (parts0 > 0) {
             add_parts(at0, parts0);
@@ -140,10 +147,10 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs a) {
                     tiles = max((hi - lo + a.chunk - 1) / a.chunk, 1);
                 }
                 if (!a.by_slot && tiles == 1) tiles = 0;                         // stored where it belongs already
-                const int end = wave_sums(tiles, lane);
                 bool match = tiles > 0 && hi > lo;
                 if (a.by_slot) match = match && slot_of(a.slots, a.n_slots, e) == matrix;
                 else match = match && e == matrix;
+                const int end = wave_sums(tiles, lane);
                 uint64_t set = __ballot(match);
                 while (set) {
                     const int g = __builtin_ctzll(set);
@@ -160,10 +167,17 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs a) {
         if (!mine) return;                                                       // the same in all four waves
         sums[wave][lane] = sum;
         __syncthreads();
-        if (wave == 0 && in) {
+        if (wave == 0 && room > 0) {
             float* out = a.out + (int64_t)matrix * a.size + at;
-            const float total = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-            *out = a.accumulate ? *out + total : total;
+            v4f total = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            if (fours) {
+                if (a.accumulate) total += *reinterpret_cast<const v4f*>(out);
+                *reinterpret_cast<v4f*>(out) = total;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < room) out[e] = a.accumulate ? out[e] + total[e] : total[e];
+            }
         }
         __syncthreads();
     }
@@ -209,7 +223,7 @@ int64_t partial_count(int groups, int64_t n, int64_t splits, bool by_slot) {
 template <class Left, class Right, bool HALF, int OUTER, int INNER>
 void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
     constexpr int kTerms = Left::kTerms > Right::kTerms ? Left::kTerms : Right::kTerms;
-    constexpr int kDepth = kTerms > 1 ? 32 : 64, kBufs = kTerms > 1 ? 1 : 2;
+    constexpr int kDepth = kTerms > 2 || OUTER * INNER > 64 * 128 ? (kTerms > 1 ? 32 : 64) : 64, kBufs = kTerms > 1 ? 1 : 2;
     matrix_sums_kernel<Left, Right, HALF, OUTER, INNER, kDepth, kBufs><<<grid, 256, 0, st>>>(a);
 }
 
@@ -290,8 +304,8 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     j.chunk = a.chunk;
     j.size = (int64_t)m.outer * m.inner;
     // most groups of a large matrix are one chunk and have nothing to join: few workgroups find that out
-    const int64_t matrices = m.by_slot ? m.n_slots : count, most = (8192 + matrices - 1) / matrices;
-    j.blocks = (int)((j.size + 63) / 64 < most ? (j.size + 63) / 64 : most);
+    const int64_t matrices = m.by_slot ? m.n_slots : count, most = (2048 + matrices - 1) / matrices;
+    j.blocks = (int)((j.size + 255) / 256 < most ? (j.size + 255) / 256 : most);
     j.partial = m.partial;
     j.partials = a.partials;
     j.out = m.out;

@@ -170,12 +170,14 @@ __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
         const RowTile now = t;
         const int now_col = col0, next = ADAPT ? -1 : pieces.take();
         if (next >= 0) place(next, col0, t);
+        Segments segments = {};
+        if (ADAPT) segments.begin(a, now, lane);
         contract<DT == kTypeF16, MatrixTile, DataTile>(a.steps / kDepth, fetch, [](unsigned char*) {}, stages, wc, wr, lane, acc);
         if (next >= 0) {
             begin();
             fetch(left0, right0, true);
         }
-        finish_rows<DT, BACKWARD, ADAPT, 4, 2, ONCE>(a, now, now_col + 128 * wc, 64 * wr, acc, wave < 4 ? left1 : right1, wave & 3, lane, loaded);
+        finish_rows<DT, BACKWARD, ADAPT, 4, 2, ONCE>(a, now, segments, now_col + 128 * wc, 64 * wr, acc, wave < 4 ? left1 : right1, wave & 3, lane, loaded);
         if (next < 0) break;
     }
 }
