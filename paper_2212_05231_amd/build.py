@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libneus2.so")
 SOURCES = ["api.hip", "hash_grid.hip", "sdf_mlp.hip", "color_mlp.hip", "render.hip", "occupancy.hip",
-           "layers.hip", "layers_grad.hip", "layers_wide.hip"]
+           "layers.hip", "layers_grad.hip", "layers_wide.hip",
+           "layers_narrow.hip"]
 # the ray marcher decides integers from binary32 arithmetic: one rounding per operation there
 EXTRA_FLAGS = {"occupancy.hip": ["-ffp-contract=off"]}
 # packed fp32 instructions are switched off on purpose (the compiler otherwise forms them at -O3)

@@ -703,6 +703,10 @@ struct MatrixGradient {
 };
 int64_t matrix_gradient_bytes(const MatrixGradient& m);
 int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st);
+bool narrow_backward_fits(int dtype, int inner, int outer, int64_t groups, int64_t n, int64_t dy_stride, int64_t x_stride, bool packed);
+int64_t narrow_backward_bytes(int inner, int outer, int64_t groups);
+int launch_narrow_backward(int dtype, const RowsArgs& rows, const MatrixGradient& m, hipStream_t st);      // rows.y NULL: no dx
+int launch_adapter_gradients(const MatrixGradient& da, const MatrixGradient& db, hipStream_t st);       // by slot both
 
 inline int element_bytes(int dtype) { return dtype == kTypeF32 ? 4 : 2; }
 

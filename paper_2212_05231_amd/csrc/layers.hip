@@ -702,7 +702,10 @@ int64_t neus2_grouped_workspace_bytes(const neus2_layer* l, int64_t n) {
     m.groups = make_groups(nullptr, l->groups, n, false);
     m.dtype = l->dtype;
     m.outer = l->out_dim; m.inner = l->in_dim;
-    return matrix_gradient_bytes(m);
+    // whether the input comes in 8 bits is not known here, and decides only together with its stride
+    const int64_t sums = matrix_gradient_bytes(m), narrow = narrow_backward_bytes(l->in_dim, l->out_dim, l->groups);
+    const bool fits = narrow_backward_fits(l->dtype, l->in_dim, l->out_dim, l->groups, n, y_stride_of(l), x_stride_of(l), true);
+    return fits && narrow > sums ? narrow : sums;
 }
 
 int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, const uint8_t* xe, const uint32_t* masks, const void* W,
@@ -723,25 +726,27 @@ int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(NEUS2_ERR_SHAPE, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)need);
     hipStream_t st = (hipStream_t)stream;
-    if (dx && n > 0) {
-        RowsArgs a = {};
-        a.groups = make_groups(offsets, l->groups, n, false);
-        a.steps = l->out_dim; a.cols = l->in_dim;
-        a.x = dy; a.x_stride = y_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
-        a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
-        a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
-        a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
-        NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
-    }
-    if (!dW) return NEUS2_OK;
+    RowsArgs a = {};
+    a.groups = make_groups(offsets, l->groups, n, false);
+    a.steps = l->out_dim; a.cols = l->in_dim;
+    a.x = dy; a.x_stride = y_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+    a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
+    a.y = dx; a.y_stride = x_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
+    a.masks = masks; a.mask_words = (l->in_dim + 31) / 32;
+    a.once = n * l->in_dim * element_bytes(l->dtype) > kStoreOnceBytes;
+    if (!dW) return n > 0 ? launch_rows<true>(l->dtype, a, st) : NEUS2_OK;
     MatrixGradient m = {};
-    m.groups = make_groups(offsets, l->groups, n, false);
+    m.groups = a.groups;
     m.dtype = l->dtype;
-    m.dy = dy; m.dy_stride = y_stride_of(l);
-    m.x = x; m.x_stride = x_stride_of(l); m.xq = xq; m.xe = xe;
+    m.dy = dy; m.dy_stride = a.x_stride;
+    m.x = x; m.x_stride = a.y_stride; m.xq = xq; m.xe = xe;
     m.outer = l->out_dim; m.inner = l->in_dim;
     m.out = dW; m.accumulate = l->accumulate;
     m.partial = (float*)workspace;
+    // (the sums of dW alone come from the same kernel: the same bits with and without dx)
+    if (narrow_backward_fits(l->dtype, l->in_dim, l->out_dim, l->groups, n, m.dy_stride, m.x_stride, xq != nullptr))
+        return launch_narrow_backward(l->dtype, a, m, st);
+    if (dx && n > 0) NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
     return launch_matrix_gradient(m, st);
 }
 
@@ -797,7 +802,7 @@ int64_t neus2_adapter_workspace_bytes(const neus2_layer* l, int64_t n) {
     const int64_t da = matrix_gradient_bytes(m);
     m.outer = l->out_dim; m.inner = l->rank;
     const int64_t db = matrix_gradient_bytes(m);
-    return v + (da > db ? da : db);
+    return v + da + db;
 }
 
 int neus2_adapter_bwd(const neus2_layer* l, const void* x, const int8_t* xq, const uint8_t* xe, const uint32_t* masks, const void* W,
@@ -851,12 +856,13 @@ int neus2_adapter_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
     m.left = v;
     m.x = x; m.x_stride = x_stride_of(l); m.xq = xq; m.xe = xe;
     m.out = dA;
-    NEUS2_TRY(launch_matrix_gradient(m, st));
-    m.outer = l->out_dim; m.inner = l->rank;                   // dB[slot] = sum dy u^T
-    m.left = nullptr; m.dy = dy; m.dy_stride = y_stride_of(l);
-    m.right = u; m.x = nullptr; m.xq = nullptr; m.xe = nullptr;
-    m.out = dB;
-    return launch_matrix_gradient(m, st);
+    MatrixGradient b = m;
+    b.outer = l->out_dim; b.inner = l->rank;                   // dB[slot] = sum dy u^T
+    b.left = nullptr; b.dy = dy; b.dy_stride = y_stride_of(l);
+    b.right = u; b.x = nullptr; b.xq = nullptr; b.xe = nullptr;
+    b.out = dB;
+    b.partial = partial + matrix_gradient_bytes(m) / 4;
+    return launch_adapter_gradients(m, b, st);
 }
 
 static int check_pack(int dtype, int64_t n, int32_t dim, int64_t x_stride) {

@@ -19,21 +19,31 @@ __device__ __forceinline__ typename Factor::Pointer make_pointer(const void* p, 
     return f;
 }
 
-template <class Left, class Right, bool HALF, int OUTER, int INNER, int DEPTH, int BUFS>
-__global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
-    constexpr int kThreads = 256;
+// How a product of these factors is cut: k-steps a round, and one or two buffers (with several terms the tiles are large and there is
+// enough to do in a round; the other workgroups of the compute unit fill the waits).
+template <class Left, class Right, int OUTER, int INNER>
+struct SumShape {
+    static constexpr int kTerms = Left::kTerms > Right::kTerms ? Left::kTerms : Right::kTerms;
+    static constexpr int kDepth = kTerms > 2 || (kTerms > 1 && OUTER * INNER > 64 * 128) ? 32 : 64, kBufs = kTerms > 1 ? 1 : 2;
+    typedef FactorTile<Left, false, OUTER, kDepth, 256> LeftTile;
+    typedef FactorTile<Right, false, INNER, kDepth, 256> RightTile;
+    static constexpr int kBuf = LeftTile::kBytes + RightTile::kBytes, kBytes = kBufs * kBuf;
+};
+
+template <class Left, class Right, bool HALF, int OUTER, int INNER>
+__device__ __forceinline__ void matrix_sums(const SumArgs& a, int block, unsigned char* lds) {
+    typedef SumShape<Left, Right, OUTER, INNER> Shape;
+    typedef typename Shape::LeftTile LeftTile;
+    typedef typename Shape::RightTile RightTile;
+    constexpr int DEPTH = Shape::kDepth, BUFS = Shape::kBufs, kBuf = Shape::kBuf;
     constexpr int kBO = OUTER / 64, kBI = INNER / 64;            // four waves, two by two
-    typedef FactorTile<Left, false, OUTER, DEPTH, kThreads> LeftTile;
-    typedef FactorTile<Right, false, INNER, DEPTH, kThreads> RightTile;
-    constexpr int kBuf = LeftTile::kBytes + RightTile::kBytes;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[BUFS * kBuf];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wo = wave >> 1, wi = wave & 1;
     const int tiles = a.outer_tiles * a.inner_tiles;
-    const int tile = (int)(blockIdx.x % tiles);
+    const int tile = block % tiles;
     const int outer0 = tile / a.inner_tiles * OUTER, inner0 = tile % a.inner_tiles * INNER;
-    const RowTile t = locate<true>(a.groups, a.chunk, 1, (int)(blockIdx.x / tiles), lane);
+    const RowTile t = locate<true>(a.groups, a.chunk, 1, block / tiles, lane);
     if (t.group < 0) return;
 
     const typename Left::Pointer left = make_pointer<Left>(a.left, nullptr, a.left_stride, a.left_whole);
@@ -89,6 +99,23 @@ __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
     store_sums<false, kBO, kBI>(a, t, outer0 + 32 * wo * kBO, inner0 + 32 * wi * kBI, acc, lane);
 }
 
+template <class Left, class Right, bool HALF, int OUTER, int INNER>
+__global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
+    __shared__ __attribute__((aligned(16))) unsigned char lds[SumShape<Left, Right, OUTER, INNER>::kBytes];
+    matrix_sums<Left, Right, HALF, OUTER, INNER>(a, (int)blockIdx.x, lds);
+}
+
+// Both narrow matrices of adapters, dA (v x^T) and dB (dy u^T), in one launch: each alone is a row of waits (8192 rows, 2048 wide, rank
+// 16: 14.4 us each).  WIDE: tiles of 128 along the long side of both.
+template <class V, class X, class Dy, class U, int WIDE>
+__global__ __launch_bounds__(256) void adapter_sums_kernel(SumArgs a, SumArgs b, int blocks_a) {
+    typedef SumShape<V, X, 64, WIDE> A;
+    typedef SumShape<Dy, U, WIDE, 64> B;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[A::kBytes > B::kBytes ? A::kBytes : B::kBytes];
+    if ((int)blockIdx.x < blocks_a) matrix_sums<V, X, false, 64, WIDE>(a, (int)blockIdx.x, lds);
+    else matrix_sums<Dy, U, false, WIDE, 64>(b, (int)blockIdx.x - blocks_a, lds);
+}
+
 // Adds the chunks' sums.  A workgroup has 256 elements of one matrix; each of its four waves adds every fourth chunk in the order of
 // the rows, then the four sums are added, so the order is always the same.
 struct JoinArgs {
@@ -101,15 +128,18 @@ struct JoinArgs {
     int by_slot; const int32_t* slots; int n_slots;
 };
 
-__global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs a) {
+__global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs one, JoinArgs two, int blocks_one) {
     __shared__ v4f sums[4][64];
+    const bool second = (int)blockIdx.x >= blocks_one;
+    const JoinArgs& a = second ? two : one;
+    const int block = (int)blockIdx.x - (second ? blocks_one : 0);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int matrix = (int)(blockIdx.x / a.blocks);
+    const int matrix = block / a.blocks;
     const int groups = a.groups.offsets ? a.groups.groups : 1;
     const bool fours = a.size % 4 == 0;
     int at0 = 0, parts0 = 0;                                                     // a group's parts, if there is only one group
     bool mine = a.by_slot != 0;
-    for (int64_t first = (int64_t)(blockIdx.x % a.blocks) * 256; first < a.size; first += (int64_t)a.blocks * 256) {
+    for (int64_t first = (int64_t)(block % a.blocks) * 256; first < a.size; first += (int64_t)a.blocks * 256) {
         const int64_t at = first + 4 * lane;
         const int room = (int)min((int64_t)4, a.size - at);                      // of this lane's four elements, how many there are
         v4f sum = {0.f, 0.f, 0.f, 0.f};
@@ -220,20 +250,13 @@ int64_t partial_count(int groups, int64_t n, int64_t splits, bool by_slot) {
     return splits == 1 || n <= kLeastChunk ? 0 : 2 * chunks;
 }
 
-template <class Left, class Right, bool HALF, int OUTER, int INNER>
-void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
-    constexpr int kTerms = Left::kTerms > Right::kTerms ? Left::kTerms : Right::kTerms;
-    constexpr int kDepth = kTerms > 2 || OUTER * INNER > 64 * 128 ? (kTerms > 1 ? 32 : 64) : 64, kBufs = kTerms > 1 ? 1 : 2;
-    matrix_sums_kernel<Left, Right, HALF, OUTER, INNER, kDepth, kBufs><<<grid, 256, 0, st>>>(a);
-}
-
 template <class Left, class Right, bool HALF>
 void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
     const bool o = a.outer > 64, i = a.inner > 64;
-    if (o && i) launch_sums<Left, Right, HALF, 128, 128>(a, grid, st);
-    else if (o) launch_sums<Left, Right, HALF, 128, 64>(a, grid, st);
-    else if (i) launch_sums<Left, Right, HALF, 64, 128>(a, grid, st);
-    else launch_sums<Left, Right, HALF, 64, 64>(a, grid, st);
+    if (o && i) matrix_sums_kernel<Left, Right, HALF, 128, 128><<<grid, 256, 0, st>>>(a);
+    else if (o) matrix_sums_kernel<Left, Right, HALF, 128, 64><<<grid, 256, 0, st>>>(a);
+    else if (i) matrix_sums_kernel<Left, Right, HALF, 64, 128><<<grid, 256, 0, st>>>(a);
+    else matrix_sums_kernel<Left, Right, HALF, 64, 64><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -242,12 +265,16 @@ void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
 int64_t matrix_gradient_bytes(const MatrixGradient& m) {
     const bool wide = wide_sums_fit(m);
     const int64_t count = partial_count(m.groups.groups, m.groups.n, splits_of(m.outer, m.inner, wide), m.by_slot);
-    return count * m.outer * m.inner * 4;
+    return (count * m.outer * m.inner * 4 + 15) / 16 * 16;
 }
 
-int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
-    const int count = m.groups.offsets ? m.groups.groups : 1;
-    const bool wide = wide_sums_fit(m);
+namespace {
+
+int group_count(const MatrixGradient& m) { return m.groups.offsets ? m.groups.groups : 1; }
+
+// everything but the tiles
+SumArgs sum_args(const MatrixGradient& m, bool wide) {
+    const int count = group_count(m);
     const int64_t splits = splits_of(m.outer, m.inner, wide);
     SumArgs a = {};
     a.groups = m.groups;
@@ -272,23 +299,75 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     } else {
         a.right = m.x; a.right_stride = m.x_stride; a.right_whole = rows_whole(m.dtype, m.x_stride, m.inner);
     }
-    const bool f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
+    return a;
+}
+
+// the number of workgroups with tiles of this size
+int64_t cut(const MatrixGradient& m, SumArgs& a, int outer_tile, int inner_tile) {
+    a.outer_tiles = (a.outer + outer_tile - 1) / outer_tile;
+    a.inner_tiles = (a.inner + inner_tile - 1) / inner_tile;
+    return chunk_count(group_count(m), m.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles;
+}
+
+JoinArgs join_args(const MatrixGradient& m, const SumArgs& a, int64_t& blocks) {
+    JoinArgs j = {};
+    j.groups = m.groups;
+    j.chunk = a.chunk;
+    j.size = (int64_t)m.outer * m.inner;
+    // most groups of a large matrix are one chunk and have nothing to join: few workgroups find that out
+    const int64_t matrices = m.by_slot ? m.n_slots : group_count(m), most = (2048 + matrices - 1) / matrices;
+    j.blocks = (int)((j.size + 255) / 256 < most ? (j.size + 255) / 256 : most);
+    j.partial = m.partial;
+    j.partials = a.partials;
+    j.out = m.out;
+    j.accumulate = m.accumulate;
+    j.by_slot = a.by_slot;
+    j.slots = m.slots;
+    j.n_slots = m.n_slots;
+    blocks = matrices * j.blocks;
+    return j;
+}
+
+template <class V, class X, class Dy, class U>
+void launch_adapter_sums(const SumArgs& a, const SumArgs& b, bool wide, int64_t blocks_a, int64_t blocks, hipStream_t st) {
+    if (wide) adapter_sums_kernel<V, X, Dy, U, 128><<<(unsigned)blocks, 256, 0, st>>>(a, b, (int)blocks_a);
+    else adapter_sums_kernel<V, X, Dy, U, 64><<<(unsigned)blocks, 256, 0, st>>>(a, b, (int)blocks_a);
+}
+
+}  // namespace
+
+int launch_adapter_gradients(const MatrixGradient& da, const MatrixGradient& db, hipStream_t st) {
+    SumArgs a = sum_args(da, false), b = sum_args(db, false);
+    const bool wide = da.inner > 64 || db.outer > 64;
+    const int64_t blocks_a = cut(da, a, 64, wide ? 128 : 64), blocks = blocks_a + cut(db, b, wide ? 128 : 64, 64);
+    NEUS2_TRY(check_grid(blocks));
+    if (da.dtype == kTypeF32) {
+        if (da.xq) launch_adapter_sums<Wide<3>, Packed<false>, Wide<3>, Wide<3>>(a, b, wide, blocks_a, blocks, st);
+        else launch_adapter_sums<Wide<3>, Wide<3>, Wide<3>, Wide<3>>(a, b, wide, blocks_a, blocks, st);
+    } else if (da.dtype == kTypeF16) {
+        if (da.xq) launch_adapter_sums<Wide<2>, Packed<false>, HalfPair, Wide<2>>(a, b, wide, blocks_a, blocks, st);
+        else launch_adapter_sums<Wide<2>, HalfPair, HalfPair, Wide<2>>(a, b, wide, blocks_a, blocks, st);
+    } else {
+        if (da.xq) launch_adapter_sums<Wide<2>, Packed<false>, Native, Wide<2>>(a, b, wide, blocks_a, blocks, st);
+        else launch_adapter_sums<Wide<2>, Native, Native, Wide<2>>(a, b, wide, blocks_a, blocks, st);
+    }
+    NEUS2_TRY(check_launch("adapter gradients"));
+    int64_t joins_a, joins_b;
+    const JoinArgs ja = join_args(da, a, joins_a), jb = join_args(db, b, joins_b);
+    NEUS2_TRY(check_grid(joins_a + joins_b));
+    join_sums_kernel<<<(unsigned)(joins_a + joins_b), 256, 0, st>>>(ja, jb, (int)joins_a);
+    return check_launch("adapter gradient sums");
+}
+
+int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
+    const bool wide = wide_sums_fit(m), f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
     const bool aligned = rows_aligned(m.dtype, m.dy_stride) && m.dy_stride <= (1 << 20) &&
                          (m.xq || (rows_aligned(m.dtype, m.x_stride) && m.x_stride <= (1 << 20)));
-    const int to = wide && aligned ? kWideOuter : tile_of(m.outer), ti = wide && aligned ? kWideInner : tile_of(m.inner);
-    a.outer_tiles = (a.outer + to - 1) / to;
-    a.inner_tiles = (a.inner + ti - 1) / ti;
-    const int64_t blocks = chunk_count(count, m.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles;
+    SumArgs a = sum_args(m, wide);
+    const int64_t blocks = cut(m, a, wide && aligned ? kWideOuter : tile_of(m.outer), wide && aligned ? kWideInner : tile_of(m.inner));
     NEUS2_TRY(check_grid(blocks));
     const unsigned grid = (unsigned)blocks;
-    if (m.left) {                                                       // v x^T
-        if (f32) m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
-        else if (m.xq) launch_sums<Wide<2>, Packed<false>, false>(a, grid, st);
-        else f16 ? launch_sums<Wide<2>, HalfPair, false>(a, grid, st) : launch_sums<Wide<2>, Native, false>(a, grid, st);
-    } else if (m.right) {                                               // dy u^T
-        if (f32) launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
-        else f16 ? launch_sums<HalfPair, Wide<2>, false>(a, grid, st) : launch_sums<Native, Wide<2>, false>(a, grid, st);
-    } else if (f32) {
+    if (f32) {
         m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
     } else if (wide && aligned) {
         launch_wide_sums(m.dtype, m.xq != nullptr, a, grid, st);
@@ -299,23 +378,10 @@ int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     }
     NEUS2_TRY(check_launch("matrix gradient"));
     if (a.partials == 0) return NEUS2_OK;                               // every group was one chunk
-    JoinArgs j = {};
-    j.groups = m.groups;
-    j.chunk = a.chunk;
-    j.size = (int64_t)m.outer * m.inner;
-    // most groups of a large matrix are one chunk and have nothing to join: few workgroups find that out
-    const int64_t matrices = m.by_slot ? m.n_slots : count, most = (2048 + matrices - 1) / matrices;
-    j.blocks = (int)((j.size + 255) / 256 < most ? (j.size + 255) / 256 : most);
-    j.partial = m.partial;
-    j.partials = a.partials;
-    j.out = m.out;
-    j.accumulate = m.accumulate;
-    j.by_slot = a.by_slot;
-    j.slots = m.slots;
-    j.n_slots = m.n_slots;
-    const int64_t joins = matrices * j.blocks;
+    int64_t joins;
+    const JoinArgs j = join_args(m, a, joins);
     NEUS2_TRY(check_grid(joins));
-    join_sums_kernel<<<(unsigned)joins, 256, 0, st>>>(j);
+    join_sums_kernel<<<(unsigned)joins, 256, 0, st>>>(j, j, (int)joins);
     return check_launch("matrix gradient sums");
 }
 

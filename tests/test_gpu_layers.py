@@ -129,6 +129,39 @@ def test_grouped_backward(shape, dtype, packed, use_masks, accumulate):
     assert torch.equal(dx2.contiguous(), dx.contiguous()) and torch.equal(dW2, dW)
 
 
+@pytest.mark.parametrize("packed,use_masks,accumulate", [(False, False, 1), (True, True, 0)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,groups,inner,outer", [(65536, 1, 64, 64), (70011, 20, 64, 64), (66000, 200, 32, 8), (65600, 7, 40, 48)])
+def test_narrow_layers_backward_in_one_pass(n, groups, inner, outer, dtype, packed, use_masks, accumulate):
+    """Many rows of a narrow layer: runs of rows that begin and end inside groups, groups without rows, rows of nobody; with and
+    without dx the same sums."""
+    gen = torch.Generator().manual_seed(n)
+    off = split_rows(n, groups, gen, 37 if groups > 1 else 0, 41 if groups > 1 else 0, groups // 5)
+    x, dy = rows(n, inner, inner, dtype, gen, relu=use_masks), rows(n, outer, outer, dtype, gen, scale=0.01)
+    x[:off[0]], dy[:off[0]] = float("nan"), float("inf")
+    W = (torch.randn(groups, outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    layer = nb.make_layer(dtype, groups, inner, outer, accumulate=bool(accumulate))
+    q8, e8, mask = (torch.zeros(n, (inner + 31) // 32 * 32, dtype=torch.int8, device="cuda"),
+                    torch.zeros(n, (inner + 31) // 32, dtype=torch.uint8, device="cuda"),
+                    torch.zeros(n, (inner + 31) // 32, dtype=torch.int32, device="cuda"))
+    nb.pack8(x, q8, e8, mask)                                    # held to the definition by test_pack_and_unpack
+    x64 = lo.unpack8(q8.cpu().numpy(), e8.cpu().numpy(), inner) if packed else f64(x)
+    workspace = torch.full((nb.grouped_workspace_bytes(layer, n) // 4,), float("nan"), device="cuda")
+    dx, dW = empty(n, inner, inner, dtype), torch.full((groups, outer, inner), 0.5, device="cuda")
+    given, masks = (q8, e8) if packed else x, mask if use_masks else None
+    nb.grouped_bwd(layer, given, W, on_device(off), dy, dx, dW, workspace, masks=masks)
+    want_dx, want_dW = lo.grouped_backward(x64, f64(W), off, f64(dy), f64(x) > 0 if use_masks else None)
+    size_dx, size_dW = lo.grouped_backward(np.abs(nan_to(x64)), np.abs(f64(W)), off, np.abs(np.where(np.isinf(f64(dy)), 0.0, f64(dy))))
+    check(dx, want_dx, size_dx, dtype, outer, "dx")
+    start = 0.5 if accumulate else 0.0
+    most = max(off[g + 1] - off[g] for g in range(groups))
+    check(dW, want_dW + start, size_dW + start, "f32", most, "dW", extra=0.0 if not accumulate else 1e-30)
+    dW2, dx2 = torch.full((groups, outer, inner), 0.5, device="cuda"), empty(n, inner, inner, dtype)
+    nb.grouped_bwd(layer, given, None, on_device(off), dy, None, dW2, workspace)
+    nb.grouped_bwd(layer, None, W, on_device(off), dy, dx2, None, masks=masks)
+    assert torch.equal(dW, dW2) and torch.equal(dx, dx2)
+
+
 def test_one_group_without_offsets_and_many_chunks():
     """offsets NULL; 70 000 rows of a small matrix: hundreds of chunks joined in order, bit for bit the same twice."""
     gen = torch.Generator().manual_seed(3)
