@@ -453,14 +453,15 @@ int neus2_march_rays(int log2_res, const uint32_t* bitfield, const float* origin
  * Row strides: x_stride, y_stride count values from one row to the next (0: in_dim, out_dim); dx has
  *   x's, dy has y's.  Any stride works, multiples of 16 bytes are the fast ones.
  * accumulate: matrix gradients are ADDED into (1) or overwritten (0: groups without rows get zeros).
+ * Outputs must not overlap inputs.
  * n = 0: the arrays of rows may be NULL; matrix gradients are zeroed or left as they are.
  * Results do not depend on the order in which workgroups run. */
 typedef struct neus2_layer {
     int32_t dtype;             /* 0 = fp32, 1 = fp16, 2 = bf16 */
-    int32_t groups;            /* groups of consecutive rows, 1..2^20 */
+    int32_t groups;            /* groups of consecutive rows, 1..2^16 */
     int32_t in_dim, out_dim;   /* 1..65536 */
     int32_t rank;              /* adapters: 1..64; 0 for a grouped layer */
-    int32_t adapters;          /* adapters: matrices in the bank, 1..2^20; 0 for a grouped layer */
+    int32_t adapters;          /* adapters: matrices in the bank, 1..2^16; 0 for a grouped layer */
     int32_t relu;              /* 1: y = max(W x, 0) */
     int32_t accumulate;
     int64_t x_stride, y_stride;

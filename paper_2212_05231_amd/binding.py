@@ -395,6 +395,11 @@ def _current_device(t, name) -> int:
     return device
 
 
+def _check_workspace(t, device) -> None:
+    if t is not None and (t.get_device() != device or not t.is_contiguous() or t.element_size() < 4):
+        raise ValueError("workspace: a contiguous tensor of 4-byte elements on the rows' device")
+
+
 def _device_rows(device) -> None:
     if device < 0:
         raise ValueError("the rows are in host memory")
@@ -464,6 +469,7 @@ def grouped_bwd(layer, x, W, offsets, dy, dx, dW, workspace=None, masks=None) ->
         _check_rows(dx, "dx", n, layer.in_dim, layer.x_stride, dtype, device)
     if dW is not None:
         _check_tensor(dW, "dW", (layer.groups, layer.out_dim, layer.in_dim), torch.float32, device)
+    _check_workspace(workspace, device)
     _device_rows(device)
     _check(lib().neus2_grouped_bwd(C.byref(layer), xp, xq, xe, _data(masks), _data(W), _data(offsets), _data(dy), n, _data(dx),
                                    _data(dW), _ptr(workspace), _bytes(workspace), _stream()))
@@ -514,6 +520,7 @@ def adapter_bwd(layer, x, W, A, B, scales, slots, offsets, u, dy, dx, dA, dB, wo
     for t, name, like in ((dA, "dA", A), (dB, "dB", B)):
         if t is not None:
             _check_tensor(t, name, like.shape, torch.float32, device)
+    _check_workspace(workspace, device)
     _device_rows(device)
     _check(lib().neus2_adapter_bwd(C.byref(layer), xp, xq, xe, _data(masks), _data(W), _data(A), _data(B), _data(scales), _data(slots),
                                    _data(offsets), _data(u), _data(dy), n, _data(dx), _data(dA), _data(dB), _ptr(workspace),
@@ -523,8 +530,9 @@ def adapter_bwd(layer, x, W, A, B, scales, slots, offsets, u, dy, dx, dA, dB, wo
 def _check_packed_form(q, e, masks, n, dim, device) -> None:
     import torch
     blocks = (dim + 31) // 32
-    if q is not None or e is not None or masks is None:
+    if q is not None:
         _check_tensor(q, "q", (n, 32 * blocks), torch.int8, device)
+    if e is not None:
         _check_tensor(e, "e", (n, blocks), torch.uint8, device)
     if masks is not None:
         _check_tensor(masks, "masks", (n, blocks), torch.int32, device)

@@ -716,8 +716,10 @@ inline int rows_aligned(int dtype, int64_t stride) { return (stride * element_by
 // ... and are read in whole units of eight values, through 32-bit offsets
 inline int rows_whole(int dtype, int64_t stride, int64_t length) { return rows_aligned(dtype, stride) && length % 8 == 0 && stride <= (1 << 20); }
 
+// at most this many tiles of at least one row
 inline int64_t row_tiles(const RowGroups& g, int rows) {
-    return ((int64_t)g.n + rows - 1) / rows + (g.offsets && !g.whole ? g.groups : 0);
+    const int64_t tiles = ((int64_t)g.n + rows - 1) / rows + (g.offsets && !g.whole ? g.groups : 0);
+    return tiles < g.n ? tiles : g.n;
 }
 
 inline int check_grid(int64_t blocks) {

@@ -632,7 +632,7 @@ int64_t y_stride_of(const neus2_layer* l) { return l->y_stride ? l->y_stride : l
 int check_layer(const neus2_layer* l, bool adapters) {
     if (!l) return fail(NEUS2_ERR_NULL, "layer is NULL");
     if (l->dtype < 0 || l->dtype > 2) return fail(NEUS2_ERR_CONFIG, "dtype = %d, must be 0 (fp32), 1 (fp16) or 2 (bf16)", l->dtype);
-    if (l->groups < 1 || l->groups > (1 << 20)) return fail(NEUS2_ERR_CONFIG, "groups = %d, must be 1..2^20", l->groups);
+    if (l->groups < 1 || l->groups > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "groups = %d, must be 1..2^16", l->groups);
     if (l->in_dim < 1 || l->in_dim > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "in_dim = %d, must be 1..65536", l->in_dim);
     if (l->out_dim < 1 || l->out_dim > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "out_dim = %d, must be 1..65536", l->out_dim);
     if (l->x_stride != 0 && (l->x_stride < l->in_dim || l->x_stride > (1 << 24)))
@@ -643,7 +643,7 @@ int check_layer(const neus2_layer* l, bool adapters) {
     if (l->accumulate != 0 && l->accumulate != 1) return fail(NEUS2_ERR_CONFIG, "accumulate = %d, must be 0 or 1", l->accumulate);
     if (adapters) {
         if (l->rank < 1 || l->rank > 64) return fail(NEUS2_ERR_UNSUPPORTED, "rank = %d, kernels exist for 1..64", l->rank);
-        if (l->adapters < 1 || l->adapters > (1 << 20)) return fail(NEUS2_ERR_CONFIG, "adapters = %d, must be 1..2^20", l->adapters);
+        if (l->adapters < 1 || l->adapters > (1 << 16)) return fail(NEUS2_ERR_CONFIG, "adapters = %d, must be 1..2^16", l->adapters);
     } else if (l->rank != 0 || l->adapters != 0) {
         return fail(NEUS2_ERR_CONFIG, "rank = %d, adapters = %d: a grouped layer has no adapters", l->rank, l->adapters);
     }

@@ -200,6 +200,57 @@ def test_infinities_and_nan_stay_in_their_rows():
         assert torch.equal(y[keep], z[keep])
 
 
+@pytest.mark.parametrize("n,inner,outer,rank", [(40, 64, 48, 8), (300, 64, 64, 8), (600, 256, 256, 16), (600, 64, 320, 40)])
+def test_an_infinite_adapter_stays_with_its_rows(n, inner, outer, rank):
+    """Segments that share tiles: what is not finite in one adapter's matrices reaches its own rows and gradients only."""
+    for dtype in ("f32", "f16", "bf16"):
+        gen = torch.Generator().manual_seed(n + rank)
+        x, dy = rows(n, inner, inner, dtype, gen), rows(n, outer, outer, dtype, gen, 0.01)
+        W = (torch.randn(outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+        A = (torch.randn(3, rank, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+        B = (torch.randn(3, outer, rank, generator=gen) * rank ** -0.5).to(TYPES[dtype]).cuda()
+        scales = torch.ones(3, device="cuda")
+        off, slots = [0, n // 3 + 1, n // 2 + 1, n], [0, 1, 2]
+        layer = nb.make_layer(dtype, 3, inner, outer, rank=rank, adapters=3)
+        workspace = torch.zeros(nb.adapter_workspace_bytes(layer, n) // 4, device="cuda")
+        results = []
+        for poison in (False, True):
+            if poison:
+                A[1, 0, 0], B[1, 1, 0], B[1, 2, 1] = float("nan"), float("inf"), -float("inf")
+            y, u, dx = empty(n, outer, outer, dtype), torch.zeros(n, rank, device="cuda"), empty(n, inner, inner, dtype)
+            dA, dB = torch.zeros(A.shape, device="cuda"), torch.zeros(B.shape, device="cuda")
+            nb.adapter_fwd(layer, x, W, A, B, scales, on_device(slots), on_device(off), u, y)
+            nb.adapter_bwd(layer, x, W, A, B, scales, on_device(slots), on_device(off), u, dy, dx, dA, dB, workspace)
+            results.append((y, u, dx, dA, dB))
+        others = torch.ones(n, dtype=torch.bool)
+        others[off[1]:off[2]] = False
+        for a, b in zip(results[0][:3], results[1][:3]):
+            assert torch.equal(a[others.cuda()], b[others.cuda()]) and not torch.equal(a, b)
+        for a, b in zip(results[0][3:], results[1][3:]):
+            assert torch.equal(a[[0, 2]], b[[0, 2]]) and not torch.equal(a[1], b[1])
+
+
+def test_more_groups_than_rows():
+    """5000 groups for 300 rows, most of them without any."""
+    gen = torch.Generator().manual_seed(6)
+    n, inner, outer, groups = 300, 40, 24, 5000
+    off = torch.sort(torch.randint(0, n + 1, (groups - 1,), generator=gen)).values.tolist()
+    off = [0] + off + [n]
+    x, dy = rows(n, inner, inner, "bf16", gen), rows(n, outer, outer, "bf16", gen, 0.01)
+    W = (torch.randn(groups, outer, inner, generator=gen) * inner ** -0.5).bfloat16().cuda()
+    layer = nb.make_layer("bf16", groups, inner, outer)
+    y, dx, dW = empty(n, outer, outer, "bf16"), empty(n, inner, inner, "bf16"), torch.ones(groups, outer, inner, device="cuda")
+    need = nb.grouped_workspace_bytes(layer, n) // 4
+    nb.grouped_fwd(layer, x, W, on_device(off), y)
+    nb.grouped_bwd(layer, x, W, on_device(off), dy, dx, dW, torch.zeros(need, device="cuda") if need else None)
+    magnitudes = [np.abs(f64(t)) for t in (x, W, dy)]
+    want_dx, want_dW = lo.grouped_backward(f64(x), f64(W), off, f64(dy))
+    size_dx, size_dW = lo.grouped_backward(magnitudes[0], magnitudes[1], off, magnitudes[2])
+    check(y, lo.grouped_forward(f64(x), f64(W), off), lo.grouped_forward(magnitudes[0], magnitudes[1], off), "bf16", inner, "y")
+    check(dx, want_dx, size_dx, "bf16", outer, "dx")
+    check(dW, want_dW, size_dW, "f32", n, "dW")
+
+
 def test_wrong_offsets_stay_inside_the_arrays():
     """Offsets beyond the rows, negative or decreasing: results are whatever they are, but only inside the outputs."""
     gen = torch.Generator().manual_seed(5)
@@ -225,7 +276,7 @@ def test_wrong_offsets_stay_inside_the_arrays():
 ADAPTERS = [  # n, groups, slots, inner, outer, rank, pad, before, behind
     (1, 1, 1, 1, 1, 1, 0, 0, 0), (3, 3, 2, 40, 20, 4, 0, 0, 0), (64, 64, 9, 200, 72, 16, 0, 0, 0), (61, 5, 3, 96, 136, 5, 3, 4, 3),
     (65, 65, 40, 64, 64, 8, 0, 0, 0), (500, 7, 7, 64, 64, 8, 0, 3, 9), (700, 3, 5, 136, 200, 64, 8, 0, 0), (1500, 100, 30, 300, 129, 33, 1, 1, 1),
-    (2000, 2, 2, 640, 64, 16, 0, 0, 0)]
+    (2000, 2, 2, 640, 64, 16, 0, 0, 0), (900, 9, 4, 256, 300, 20, 0, 5, 0), (1100, 150, 6, 320, 512, 64, 0, 0, 2)]
 
 
 def adapter_case(shape, dtype, seed):

@@ -45,7 +45,7 @@ def broken(**fields):
 
 
 @pytest.mark.parametrize("fields,code", [
-    (dict(dtype=3), -3), (dict(dtype=-1), -3), (dict(groups=0), -3), (dict(groups=(1 << 20) + 1), -3), (dict(in_dim=0), -3),
+    (dict(dtype=3), -3), (dict(dtype=-1), -3), (dict(groups=0), -3), (dict(groups=(1 << 16) + 1), -3), (dict(in_dim=0), -3),
     (dict(in_dim=65537), -3), (dict(out_dim=0), -3), (dict(out_dim=65537), -3), (dict(x_stride=19), -2), (dict(y_stride=11), -2),
     (dict(x_stride=(1 << 24) + 1), -2), (dict(relu=2), -3), (dict(accumulate=2), -3), (dict(rank=4), -3), (dict(adapters=1), -3)])
 def test_descriptors_of_grouped_layers(fields, code):
@@ -55,7 +55,7 @@ def test_descriptors_of_grouped_layers(fields, code):
     assert nb.grouped_workspace_bytes(l, 100) == -1
 
 
-@pytest.mark.parametrize("fields,code", [(dict(rank=0), -5), (dict(rank=65), -5), (dict(adapters=0), -3), (dict(adapters=(1 << 20) + 1), -3)])
+@pytest.mark.parametrize("fields,code", [(dict(rank=0), -5), (dict(rank=65), -5), (dict(adapters=0), -3), (dict(adapters=(1 << 16) + 1), -3)])
 def test_descriptors_of_adapter_layers(fields, code):
     l = layer(rank=8, adapters=3)
     for name, v in fields.items():
@@ -83,8 +83,8 @@ def test_pointers_and_sizes_of_grouped_layers():
     assert need > 0
     assert grouped_bwd(l, n=1 << 18, size=need - 1) == -2 and grouped_bwd(l, n=1 << 18, ws=None, size=0) == -2
     assert b"workspace" in nb.lib().neus2_last_error()
-    wide = layer(dtype="bf16", groups=1 << 20, out_dim=65536)                      # more workgroups than a launch can have
-    assert grouped_fwd(wide, n=1 << 24) == -2 and b"workgroups" in nb.lib().neus2_last_error()
+    wide = layer(dtype="bf16", groups=1 << 16, out_dim=65536, in_dim=65536)          # more workgroups than a launch can have
+    assert grouped_bwd(wide, dx=None, n=1 << 16) == -2 and b"workgroups" in nb.lib().neus2_last_error()
 
 
 def test_pointers_and_sizes_of_adapter_layers():
@@ -172,6 +172,8 @@ def test_the_binding_names_the_wrong_tensor():
         nb.make_layer("f64", 1, 4, 4)
     with pytest.raises(ValueError, match="host memory"):
         nb.grouped_fwd(l, x, W, off, y)
+    with pytest.raises(ValueError, match="workspace"):
+        nb.grouped_bwd(l, x, W, off, y, x, W, torch.zeros(64, dtype=torch.float16))
     with pytest.raises(ValueError, match="host memory"):
         nb.pack8(x, torch.zeros(8, 32, dtype=torch.int8), torch.zeros(8, 1, dtype=torch.uint8))
 
