@@ -83,22 +83,18 @@ def pack8(x, dtype):
     blocks = (dim + 31) // 32
     full = np.zeros((n, 32 * blocks))
     full[:, :dim] = x
-    q, e = np.zeros((n, 32 * blocks), np.int8), np.zeros((n, blocks), np.uint8)
-    for i in range(n):
-        for b in range(blocks):
-            v = full[i, 32 * b:32 * b + 32]
-            if not np.all(np.isfinite(v)):
-                e[i, b] = 255
-                continue
-            top = np.max(np.abs(v))
-            t = -126
-            if top > 0:
-                t = max(int(np.floor(np.log2(top))) - 9, -126)
-                while np.rint(np.ldexp(top, -t)) > 127:
-                    t += 1
-            most = 63 if t == LAST_EXPONENT[dtype] else 127
-            q[i, 32 * b:32 * b + 32] = np.clip(np.rint(np.ldexp(v, -t)), -most, most).astype(np.int8)
-            e[i, b] = t + 127
+    v = full.reshape(n, blocks, 32)
+    finite = np.all(np.isfinite(v), axis=2)
+    v = np.where(finite[..., None], v, 0.0)
+    top = np.max(np.abs(v), axis=2)
+    with np.errstate(divide="ignore"):
+        t = np.where(top > 0, np.floor(np.log2(top)) - 9, -126.0)
+    t = np.maximum(t, -126).astype(np.int64)
+    while np.any(np.rint(np.ldexp(top, -t)) > 127):
+        t += np.rint(np.ldexp(top, -t)) > 127
+    most = np.where(t == LAST_EXPONENT[dtype], 63, 127)[..., None]
+    q = np.clip(np.rint(np.ldexp(v, -t[..., None])), -most, most).astype(np.int8).reshape(n, -1)
+    e = np.where(finite, t + 127, 255).astype(np.uint8)
     with np.errstate(invalid="ignore"):
         return q, e, x > 0
 

@@ -3,9 +3,9 @@
 //
 // Types.  bf16 and fp16 factors go to the matrix cores as they are, one instruction per k-step, accumulated in fp32.  fp32
 // factors are sums of bf16 terms as in mfma_tile.h: three terms and six products, as accurate as an fp32 product.  Where a
-// factor kept in fp32 (an adapter's u or v) meets one of 16 bits, the fp32 one takes two terms (2^-17 relative, below the
-// 2^-9 or 2^-12 with which the other factor came) and an fp16 one is two bf16 terms (8 + 8 >= 11 bits: exact), so that
-// small gradients do not fall out of fp16's range.  An infinite fp32 factor makes its products NaN (inf - inf in the split).
+// factor kept in fp32 (an adapter's u or v) meets one of 16 bits, an fp16 one is two bf16 terms (8 + 8 >= 11 bits: exact), so
+// that small gradients do not fall out of fp16's range; the fp32 one takes three terms where the result is fp32 (dA, dB), and
+// two (2^-17 relative) where it is rounded to 16 bits (y, dx).  An infinite fp32 factor makes its products NaN (inf - inf in the split).
 #pragma once
 
 #include "common.h"

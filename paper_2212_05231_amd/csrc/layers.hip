@@ -537,6 +537,12 @@ int launch_rows(RowsArgs a, hipStream_t st) {
         const int64_t tiles = row_tiles(a.groups, kNarrowRows);
         const unsigned grid = (unsigned)persistent_blocks((const void*)narrow_rows_kernel<DT, BACKWARD, ONCE>, 256, tiles);
         narrow_rows_kernel<DT, BACKWARD, ONCE><<<grid, 256, 0, st>>>(a);
+    } else if (row_tiles(a.groups, 128) * ((a.cols + 127) / 128) < 2 * compute_units()) {
+        // too few tiles of 128 x 128 to hide each other's waits (2048 to 2048: bf16 2^9 rows 24 us against 33, 2^11 rows 37 against 42, 2^12
+        // rows 71 against 48; fp32 2^11 rows 126 against 138, 2^12 rows 255 against 185)
+        a.col_tiles = (a.cols + 63) / 64;
+        NEUS2_TRY(check_grid(row_tiles(a.groups, 64) * a.col_tiles));
+        rows_kernel<DT, BACKWARD, ADAPT, ONCE, 64, 64, 2, 1, kDepth, kBufs><<<dim3((unsigned)(row_tiles(a.groups, 64) * a.col_tiles)), 128, 0, st>>>(a);
     } else if (a.cols > 64) {
         a.col_tiles = (a.cols + 127) / 128;
         NEUS2_TRY(check_grid(row_tiles(a.groups, 128) * a.col_tiles));
@@ -554,10 +560,13 @@ int launch_rows(const RowsArgs& a, hipStream_t st) {
     return a.once ? launch_rows<DT, BACKWARD, false, true>(a, st) : launch_rows<DT, BACKWARD, false, false>(a, st);
 }
 
-// The wide form wants 16-byte rows, a contraction of whole lines, and enough 256 x 256 tiles to be worth its size.
+// The wide form wants rows and matrices in whole units, a contraction of whole lines, rows to fill its tiles with, and more tiles than
+// half the compute units (2048 to 2048, bf16: 2^13 rows, 256 tiles, 64 us against 91 with tiles of 128 x 128; 2^12 rows, 128 tiles, 49
+// against 48; 2^11 rows, 64 tiles, 47 against 37 with tiles of 64 x 64).
 bool wide_rows_fit(int dtype, const RowsArgs& a) {
     return dtype != kTypeF32 && a.x_whole && rows_aligned(dtype, a.w_stride) && a.steps % 64 == 0 && a.cols >= 256 &&
-           a.groups.n >= 128 * (a.groups.offsets && !a.groups.whole ? (int64_t)a.groups.groups : 2);
+           a.groups.n >= 128 * (a.groups.offsets && !a.groups.whole ? (int64_t)a.groups.groups : 2) &&
+           row_tiles(a.groups, 256) * ((a.cols + 255) / 256) > compute_units() / 2;
 }
 
 template <bool BACKWARD>
@@ -578,6 +587,15 @@ int launch_few(int dtype, FewArgs a, hipStream_t st) {
     else if (dtype == kTypeF16) few_rows_kernel<kTypeF16><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
     else few_rows_kernel<kTypeBF16><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
     return check_launch("layer, few rows");
+}
+
+// Up to 16 rows a group the matrices are read once, and little else.  Up to 64 rows a group reading them once for every 16 rows, from
+// a cache, still beats the tiles as long as the workgroups are few (2048 to 2048, one group of 64 rows: bf16 10 us against 23, fp32 20
+// against 81; 8 groups of 1024 to 1024: bf16 32 rows each 13.5 against 18, 64 rows 24 against 18, fp32 64 rows 38 against 49).  Narrow layers have a kernel.
+bool few_rows_fit(const neus2_layer* l, const RowGroups& g) {
+    if (g.n <= 16 * (int64_t)l->groups) return true;
+    return g.n <= 64 * (int64_t)l->groups && (l->in_dim > 64 || l->out_dim > 64) && 
+           row_tiles(g, 16) * ((l->out_dim + 15) / 16) <= (l->dtype == kTypeF32 ? 12 : 6) * compute_units();
 }
 
 RowGroups make_groups(const int32_t* offsets, int groups, int64_t n, bool whole) {
@@ -676,7 +694,7 @@ int neus2_grouped_fwd(const neus2_layer* l, const void* x, const void* W, const 
     if (n == 0) return NEUS2_OK;
     hipStream_t st = (hipStream_t)stream;
     const RowGroups groups = make_groups(offsets, l->groups, n, false);
-    if (n <= 16 * (int64_t)l->groups) {                       // 16 rows a group and fewer: the matrices are read once, and little else
+    if (few_rows_fit(l, groups)) {
         FewArgs a = {};
         a.groups = groups;
         a.steps = l->in_dim; a.cols = l->out_dim;

@@ -214,11 +214,6 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs one, JoinArgs t
 }
 
 // ---- how the work is cut --------------------------------------------------------------------------------------------------------
-// Matrices of at least 256 x 256 in 16-bit types take the wide tiles (layers_wide.hip), if memory rows begin on 16 bytes.
-bool wide_sums_fit(const MatrixGradient& m) {
-    return m.dtype != kTypeF32 && !m.left && !m.right && m.outer >= 256 && m.inner >= 256;
-}
-
 int tile_of(int dim) { return dim > 64 ? 128 : 64; }
 
 int64_t tiles_of(int outer, int inner, bool wide) {
@@ -233,6 +228,15 @@ constexpr int kLeastChunk = 256;
 int64_t splits_of(int outer, int inner, bool wide) {
     const int64_t tiles = tiles_of(outer, inner, wide);
     return tiles >= 256 ? 1 : ((wide ? 256 : 512) + tiles - 1) / tiles;
+}
+
+// Matrices of at least 256 x 256 in 16-bit types take the wide tiles (layers_wide.hip) where the groups alone give one to every compute
+// unit, or the chunks are long enough to be worth their sums (bf16: one group, 2048 x 2048, 2^12 rows 60 us against 77, 2^11 rows 48
+// against 45; 512 x 4096, 2^13 rows 59 against 66; 8 groups, 512 x 4096, 2^10 rows 24 against 27, 512 x 512, 2^14 rows 42 against 36).
+bool wide_sums_fit(const MatrixGradient& m) {
+    if (m.dtype == kTypeF32 || m.left || m.right || m.outer < 256 || m.inner < 256) return false;
+    const int64_t tiles = tiles_of(m.outer, m.inner, true), splits = splits_of(m.outer, m.inner, true);
+    return (tiles * m.groups.groups >= 256 && m.groups.n >= 128 * (int64_t)m.groups.groups) || m.groups.n >= 1024 * splits;
 }
 
 int chunk_rows(int64_t n, int64_t splits) {
@@ -345,11 +349,11 @@ int launch_adapter_gradients(const MatrixGradient& da, const MatrixGradient& db,
         if (da.xq) launch_adapter_sums<Wide<3>, Packed<false>, Wide<3>, Wide<3>>(a, b, wide, blocks_a, blocks, st);
         else launch_adapter_sums<Wide<3>, Wide<3>, Wide<3>, Wide<3>>(a, b, wide, blocks_a, blocks, st);
     } else if (da.dtype == kTypeF16) {
-        if (da.xq) launch_adapter_sums<Wide<2>, Packed<false>, HalfPair, Wide<2>>(a, b, wide, blocks_a, blocks, st);
-        else launch_adapter_sums<Wide<2>, HalfPair, HalfPair, Wide<2>>(a, b, wide, blocks_a, blocks, st);
+        if (da.xq) launch_adapter_sums<Wide<3>, Packed<false>, HalfPair, Wide<3>>(a, b, wide, blocks_a, blocks, st);
+        else launch_adapter_sums<Wide<3>, HalfPair, HalfPair, Wide<3>>(a, b, wide, blocks_a, blocks, st);
     } else {
-        if (da.xq) launch_adapter_sums<Wide<2>, Packed<false>, Native, Wide<2>>(a, b, wide, blocks_a, blocks, st);
-        else launch_adapter_sums<Wide<2>, Native, Native, Wide<2>>(a, b, wide, blocks_a, blocks, st);
+        if (da.xq) launch_adapter_sums<Wide<3>, Packed<false>, Native, Wide<3>>(a, b, wide, blocks_a, blocks, st);
+        else launch_adapter_sums<Wide<3>, Native, Native, Wide<3>>(a, b, wide, blocks_a, blocks, st);
     }
     NEUS2_TRY(check_launch("adapter gradients"));
     int64_t joins_a, joins_b;

@@ -68,7 +68,8 @@ def nan_to(a, value=0.0):
 SHAPES = [  # n, groups, inner, outer, x pad, y pad, before, behind, none
     (1, 1, 1, 1, 0, 0, 0, 0, 0), (1, 1, 64, 64, 0, 0, 0, 0, 0), (5, 3, 33, 7, 0, 0, 1, 1, 1), (48, 3, 200, 130, 0, 0, 0, 0, 1),
     (40, 8, 512, 48, 8, 0, 3, 2, 2), (129, 2, 64, 64, 0, 0, 0, 0, 0), (300, 5, 31, 65, 1, 3, 7, 9, 2), (517, 4, 64, 128, 0, 0, 0, 5, 0),
-    (1000, 70, 40, 96, 0, 4, 0, 0, 30), (700, 1, 129, 257, 7, 0, 0, 0, 0), (2051, 3, 256, 320, 0, 0, 2, 0, 1), (900, 2, 1000, 136, 24, 8, 0, 0, 0)]
+    (1000, 70, 40, 96, 0, 4, 0, 0, 30), (700, 1, 129, 257, 7, 0, 0, 0, 0), (2051, 3, 256, 320, 0, 0, 2, 0, 1), (900, 2, 1000, 136, 24, 8, 0, 0, 0),
+    (4300, 2, 256, 2050, 0, 6, 5, 3, 0), (8300, 64, 512, 512, 0, 0, 0, 0, 5)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])

@@ -138,10 +138,12 @@ def test_struct_size_against_the_c_compiler(tmp_path):
     assert int(subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout) == C.sizeof(nb.Neus2Layer)
 
 
-@pytest.mark.parametrize("groups,inner,outer,rank", [(3, 20, 12, 0), (64, 64, 64, 0), (1, 2048, 4096, 0), (24, 2048, 2048, 64), (49, 64, 64, 8)])
+@pytest.mark.parametrize("groups,inner,outer,rank", [(3, 20, 12, 0), (64, 64, 64, 0), (1, 2048, 4096, 0), (24, 2048, 2048, 64), (49, 64, 64, 8), (1, 512, 512, 0),
+                                                     (8, 512, 4096, 0), (300, 512, 512, 0), (2, 257, 300, 0), (7, 40, 64, 0)])
 def test_workspace_of_a_batch_serves_every_smaller_one(groups, inner, outer, rank):
     l = layer(groups=groups, in_dim=inner, out_dim=outer, rank=rank, adapters=groups if rank else 0)
     query = nb.adapter_workspace_bytes if rank else nb.grouped_workspace_bytes
+    l.dtype = 2 if outer >= 256 else 0
     sizes = [query(l, n) for n in sorted({0, 1, 2, 63, 64, 65, 255, 256, 257, 511, 513, 4095, 4097} | set(range(1000, 300000, 7919)))]
     assert all(a <= b for a, b in zip(sizes, sizes[1:])), sizes
 
