@@ -131,13 +131,26 @@ __device__ __forceinline__ int count_tiles(const RowGroups& g, int rows, int lea
 // read the same memory, every XCD takes a run of consecutive ones, its workgroups in turn (the grid is a multiple of eight).
 constexpr int kXcds = 8;
 struct Pieces {
-    int total, each, next_local;
-    __device__ __forceinline__ explicit Pieces(int count) : total(count), each((count + kXcds - 1) / kXcds), next_local((int)(blockIdx.x / kXcds)) {}
+    int total, each, next_local, limit;
+    __device__ __forceinline__ explicit Pieces(int count)
+        : total(count), each((count + kXcds - 1) / kXcds), next_local((int)(blockIdx.x / kXcds)), limit(each) {}
     // the next one for this workgroup, or -1
     __device__ __forceinline__ int take() {
         const int local = next_local, piece = (int)(blockIdx.x % kXcds) * each + local;
         next_local += (int)(gridDim.x / kXcds);
-        return local < each && piece < total ? piece : -1;
+        return local < limit && piece < total ? piece : -1;
+    }
+    // If the last round would leave half of an XCD's workgroups or more without a piece, it is taken out of those take() gives, and
+    // take_quarter() deals out its pieces' quarters instead (piece * 4 + quarter, or -1).
+    __device__ __forceinline__ void quarter_last_round() {
+        const int at_once = (int)(gridDim.x / kXcds), rounds = each / at_once, left = each - rounds * at_once;
+        if (rounds > 0 && left > 0 && 2 * left <= at_once) limit = rounds * at_once;
+    }
+    __device__ __forceinline__ int take_quarter(int& turn) const {
+        const int at = (int)(blockIdx.x / kXcds) + turn * (int)(gridDim.x / kXcds);
+        ++turn;
+        if (at >= 4 * (each - limit)) return -1;
+        return 4 * ((int)(blockIdx.x % kXcds) * each + limit + at / 4) + at % 4;
     }
 };
 

@@ -48,22 +48,23 @@ __device__ __forceinline__ void meet() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
-// The operands of one k-step of a wave: four blocks of 32 lines of the left factor (the instruction's first operand), two of the right.
+// The operands of one k-step of a wave: LB blocks of 32 lines of the left factor (the instruction's first operand), RB of the right.
+template <int LB, int RB>
 struct Operands {
-    u32x4 l[4], r[2];
+    u32x4 l[LB], r[RB];
     template <class LeftTile, class RightTile>
     __device__ __forceinline__ void read(const unsigned char* left, const unsigned char* right, int wl, int wr, int ks, int lane) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) l[c] = LeftTile::operand(left, 0, 4 * wl + c, ks, lane);
+        for (int c = 0; c < LB; ++c) l[c] = LeftTile::operand(left, 0, LB * wl + c, ks, lane);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) r[c] = RightTile::operand(right, 0, 2 * wr + c, ks, lane);
+        for (int c = 0; c < RB; ++c) r[c] = RightTile::operand(right, 0, RB * wr + c, ks, lane);
     }
     template <bool HALF, int FIRST, int LAST>
-    __device__ __forceinline__ void multiply(v16f (&acc)[4][2]) const {
+    __device__ __forceinline__ void multiply(v16f (&acc)[LB][RB]) const {
 #pragma unroll
         for (int c = FIRST; c < LAST; ++c)
 #pragma unroll
-            for (int d = 0; d < 2; ++d) acc[c][d] = mma32<HALF>(l[c], r[d], acc[c][d]);
+            for (int d = 0; d < RB; ++d) acc[c][d] = mma32<HALF>(l[c], r[d], acc[c][d]);
     }
 };
 
@@ -78,31 +79,31 @@ struct Stages {
 // fetch(left, right, more) issues a pair's loads (zeros if there is no more: an odd number of pairs ends with one of zeros);
 // land(right) is what a factor that does pass through registers still has to do.  The caller has issued the first pair's loads and waited
 // for them (loaded()); when this returns nobody reads either pair of buffers any more.
-template <bool HALF, class LeftTile, class RightTile, class Fetch, class Land>
+template <bool HALF, class LeftTile, class RightTile, int LB, int RB, class Fetch, class Land>
 __device__ __forceinline__ void contract(int rounds, const Fetch& fetch, const Land& land, const Stages& s, int wl, int wr, int lane,
-                                         v16f (&acc)[4][2]) {
+                                         v16f (&acc)[LB][RB]) {
     constexpr int kSteps = kDepth / 16;
-    Operands o[2];
+    Operands<LB, RB> o[2];
     land(s.right[0]);
     meet();
-    o[0].read<LeftTile, RightTile>(s.left[0], s.right[0], wl, wr, 0, lane);
+    o[0].template read<LeftTile, RightTile>(s.left[0], s.right[0], wl, wr, 0, lane);
     for (int k = 0; k < rounds; k += 2) {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
 #pragma unroll
             for (int ks = 0; ks < kSteps - 1; ++ks) {
-                o[(ks + 1) & 1].read<LeftTile, RightTile>(s.left[q], s.right[q], wl, wr, ks + 1, lane);
+                o[(ks + 1) & 1].template read<LeftTile, RightTile>(s.left[q], s.right[q], wl, wr, ks + 1, lane);
                 if (ks == 0) fetch(s.left[q ^ 1], s.right[q ^ 1], k + q + 1 < rounds);
-                o[ks & 1].multiply<HALF, 0, 4>(acc);
+                o[ks & 1].template multiply<HALF, 0, LB>(acc);
                 __builtin_amdgcn_sched_barrier(0);
             }
             land(s.right[q ^ 1]);
-            o[1].multiply<HALF, 0, 2>(acc);
+            o[1].template multiply<HALF, 0, LB / 2>(acc);
             __builtin_amdgcn_sched_barrier(0);
             loaded();
             meet();
-            o[0].read<LeftTile, RightTile>(s.left[q ^ 1], s.right[q ^ 1], wl, wr, 0, lane);
-            o[1].multiply<HALF, 2, 4>(acc);
+            o[0].template read<LeftTile, RightTile>(s.left[q ^ 1], s.right[q ^ 1], wl, wr, 0, lane);
+            o[1].template multiply<HALF, LB / 2, LB>(acc);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -124,6 +125,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
     // bands of four tiles of rows, in a band the rows fastest: the workgroups at work on an XCD share few rows and few columns
     const int row_tiles = count_tiles(a.groups, kRight, 0, lane);
     Pieces pieces(row_tiles * a.col_tiles);
+    if (!ADAPT) pieces.quarter_last_round();
     int col0 = 0;
     RowTile t;
     auto place = [&](int piece, int& col, RowTile& tile) {
@@ -179,6 +181,43 @@ __global__ __launch_bounds__(kThreads, 2) void wide_rows_kernel(RowsArgs a) {
         }
         finish_rows<DT, BACKWARD, ADAPT, 4, 2, ONCE>(a, now, segments, now_col + 128 * wc, 64 * wr, acc, wave < 4 ? left1 : right1, wave & 3, lane, loaded);
         if (next < 0) break;
+    }
+    if (ADAPT) return;
+    // Quarters of the last round's tiles, 128 x 128, a wave 64 x 32 of them, where few are left for it: 8192 rows, 2048 to 2048 in 5
+    // groups 79 us against 98 with whole tiles, 20000 rows, 2048 to 1024 backward in 8 groups 85 against 107; in whole rounds the same.
+    typedef FactorTile<Native, true, kRight / 2, kDepth, kThreads> SmallDataTile;
+    typedef FactorTile<Native, !BACKWARD, kLeft / 2, kDepth, kThreads> SmallMatrixTile;
+    WideTile<true, kRight / 2> small_dt;
+    WideTile<!BACKWARD, kLeft / 2> small_mt;
+    const int lane2 = (int)again((uint32_t)lane);                        // or what depends on it is worked out, and held, from the start
+    small_dt.begin(a.x_stride, wave, lane2);
+    small_mt.begin(a.w_stride, wave, lane2);
+    auto small_fetch = [&](unsigned char* matrix, unsigned char* data, bool more) {
+        small_dt.load(x, more ? x_bytes : 0, data, wave);
+        small_mt.load(w, more ? w_bytes : 0, matrix, wave);
+        x += kDepth;
+        x_bytes -= kDepth * 2;
+        w += w_step;
+        w_bytes -= w_step * 2;
+    };
+    for (int turn = 0;;) {
+        const int quarter = pieces.take_quarter(turn);
+        if (quarter < 0) break;
+        if (quarter >> 2 >= row_tiles * a.col_tiles) continue;
+        place(quarter >> 2, col0, t);
+        col0 += quarter & 2 ? kLeft / 2 : 0;
+        t.lo += quarter & 1 ? kRight / 2 : 0;
+        t.hi = min(t.hi, t.lo + kRight / 2);
+        if (t.lo >= t.hi || col0 >= a.cols) continue;
+        begin();
+        meet();                                                          // nobody stores out of the buffers any more
+        small_fetch(left0, right0, true);
+        loaded();
+        v16f acc[2][1];
+        acc[0][0] = zero16();
+        acc[1][0] = zero16();
+        contract<DT == kTypeF16, SmallMatrixTile, SmallDataTile>(a.steps / kDepth, small_fetch, [](unsigned char*) {}, stages, wc, wr, lane2, acc);
+        finish_rows<DT, BACKWARD, false, 2, 1, ONCE>(a, t, {}, col0 + 64 * wc, 32 * wr, acc, left1, wave, lane2, [] {});
     }
 }
 
