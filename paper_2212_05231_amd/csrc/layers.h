@@ -110,21 +110,24 @@ __device__ __forceinline__ void locate_next(const RowGroups& g, int rows, int le
     }
 }
 
-// How many tiles there are in all (locate's `rows` and `least`).
+// How many tiles there are in all (locate's `rows` and `least`).  Offsets that are not ordered may count rows many times over: never
+// more than the host has made room for (nor does locate count beyond that: it stops at the tile it looks for).
 __device__ __forceinline__ int count_tiles(const RowGroups& g, int rows, int least, int lane) {
     const int count = g.offsets && !g.whole ? g.groups : 1;
+    const int most = (g.n + rows - 1) / rows + count;
     int total = 0;
     for (int base = 0; base < count; base += 64) {
         const int e = base + lane;
         int lo = 0, hi = 0;
         if (e < count) {
             group_rows(g, e, lo, hi);
-            total += max((hi - lo + rows - 1) / rows, least);
+            total = min(total + max((hi - lo + rows - 1) / rows, least), most);      // 64 lanes of at most 2^24 + 2^16
         }
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-    return __builtin_amdgcn_readfirstlane(total);
+    total = __builtin_amdgcn_readfirstlane(total);
+    return min(total, most);
 }
 
 // Workgroups go to the eight XCDs in turn, each with an L2 of its own.  Of `total` pieces of work in an order in which neighbours
@@ -669,7 +672,7 @@ __device__ __forceinline__ float* sums_place(const SumArgs& a, const RowTile& t,
         return a.out + t.group * size;
     }
     const int index = (a.by_slot ? t.index : t.shared) + t.part;
-    return t.hi > t.lo && index < a.partials ? a.partial + index * size : nullptr;     // decreasing offsets may count too many
+    return t.hi > t.lo && index >= 0 && index < a.partials ? a.partial + index * size : nullptr;     // decreasing offsets may count too many
 }
 
 template <bool ONCE, int kBO, int kBI>

@@ -137,7 +137,8 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs one, JoinArgs t
     const int matrix = block / a.blocks;
     const int groups = a.groups.offsets ? a.groups.groups : 1;
     const bool fours = a.size % 4 == 0;
-    int at0 = 0, parts0 = 0;                                                     // a group's parts, if there is only one group
+    int64_t at0 = 0;
+    int parts0 = 0;                                                              // a group's parts, if there is only one group
     bool mine = a.by_slot != 0;
     for (int64_t first = (int64_t)(block % a.blocks) * 256; first < a.size; first += (int64_t)a.blocks * 256) {
         const int64_t at = first + 4 * lane;
@@ -152,9 +153,10 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs one, JoinArgs t
             for (int e = 0; e < 4; ++e) v[e] = e < room ? src[e] : 0.f;
             return v;
         };
-        auto add_parts = [&](int index, int parts) {
-            const int end = min(index + parts, a.partials);                      // decreasing offsets may count too many
-            int p = index + ((wave - turn) & 3);
+        auto add_parts = [&](int64_t index, int parts) {
+            const int end = (int)min(index + parts, (int64_t)a.partials);        // decreasing offsets may count too many
+            if (index >= end) return;
+            int p = (int)index + ((wave - turn) & 3);
             turn = (turn + parts) & 3;
             for (; p + 12 < end; p += 16) {
                 v4f v[4];
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs one, JoinArgs t
         if (parts0 > 0) {
             add_parts(at0, parts0);
         } else {
-            int before = 0;
+            int64_t before = 0;
             for (int base = 0; base < groups; base += 64) {
                 const int e = base + lane;
                 int lo = 0, hi = 0, tiles = 0;
@@ -185,7 +187,8 @@ __global__ __launch_bounds__(256) void join_sums_kernel(JoinArgs one, JoinArgs t
                 while (set) {
                     const int g = __builtin_ctzll(set);
                     set &= set - 1;
-                    const int parts = __builtin_amdgcn_readlane(tiles, g), index = before + __builtin_amdgcn_readlane(end, g) - parts;
+                    const int parts = __builtin_amdgcn_readlane(tiles, g);
+                    const int64_t index = before + __builtin_amdgcn_readlane(end, g) - parts;
                     add_parts(index, parts);
                     if (!a.by_slot) { at0 = index; parts0 = parts; }
                     mine = true;

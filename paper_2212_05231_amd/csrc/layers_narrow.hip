@@ -198,7 +198,8 @@ __global__ __launch_bounds__(256) void run_join_kernel(RowGroups groups, int run
     const int group = (int)(blockIdx.x / blocks), first = (int)(blockIdx.x % blocks) * 256 + 4 * lane;
     const int count = groups.offsets ? groups.groups : 1;
     const int64_t total = count_tiles(groups, kUnit, 0, lane);
-    int before = 0, mine = 0;                                            // units before the group's first one, and its own
+    int64_t before = 0;
+    int mine = 0;                                                        // units before the group's first one, and its own
     for (int base = 0; base <= group; base += 64) {
         const int e = base + lane;
         int lo = 0, hi = 0, units = 0;
@@ -215,12 +216,12 @@ __global__ __launch_bounds__(256) void run_join_kernel(RowGroups groups, int run
         }
     }
     v4f sum = {0.f, 0.f, 0.f, 0.f};
-    if (mine > 0) {
+    if (mine > 0 && total > 0) {
         // the last run that begins at or before a unit: run r begins at total * r / runs (rounded down)
-        const int64_t from = ((int64_t)(before + 1) * runs - 1) / total, to = ((int64_t)(before + mine) * runs - 1) / total;
+        const int64_t from = ((before + 1) * runs - 1) / total, to = min(((before + mine) * runs - 1) / total, (int64_t)runs - 1);
         for (int64_t run = from + wave; run <= to; run += 4) {
             const int64_t begin = total * run / runs, end = total * (run + 1) / runs;
-            if (max(begin, (int64_t)before) >= min(end, (int64_t)(before + mine))) continue;     // a run without units
+            if (max(begin, before) >= min(end, before + mine)) continue;     // a run without units
             const float* src = partial + (run + group) * size + first;
             if (size % 4 == 0) {
                 if (first < size) sum += *reinterpret_cast<const v4f*>(src);

@@ -274,6 +274,40 @@ def test_wrong_offsets_stay_inside_the_arrays():
         assert torch.all(dW[groups] == MARK) and torch.all(workspace[need:] == MARK)
 
 
+@pytest.mark.parametrize("n,groups,inner,outer,dtype", [(65600, 64, 64, 64, "f16"), (65600, 64, 64, 48, "f32"), (9000, 64, 512, 512, "bf16"),
+                                                        (700, 300, 256, 320, "bf16")])
+def test_wrong_offsets_stay_inside_the_arrays_of_every_kernel(n, groups, inner, outer, dtype):
+    """Groups that each claim all rows, or none: more tiles, units and chunks than there is room for."""
+    gen = torch.Generator().manual_seed(groups)
+    x, dy = rows(n, inner, inner, dtype, gen), rows(n, outer, outer, dtype, gen)
+    W = torch.randn(groups, outer, inner, generator=gen).to(TYPES[dtype]).cuda()
+    layer = nb.make_layer(dtype, groups, inner, outer)
+    rank, slots = 8, 5
+    adapted = nb.make_layer(dtype, groups, inner, outer, rank=rank, adapters=slots)
+    A, B = torch.randn(slots, rank, inner, generator=gen).to(TYPES[dtype]).cuda(), torch.randn(slots, outer, rank, generator=gen).to(TYPES[dtype]).cuda()
+    scales, named = torch.ones(slots, device="cuda"), on_device([g % 7 - 1 for g in range(groups)])
+    q, e = torch.zeros(n, (inner + 31) // 32 * 32, dtype=torch.int8, device="cuda"), torch.full((n, (inner + 31) // 32), 127, dtype=torch.uint8, device="cuda")
+    for off in ([0 if g % 2 else n for g in range(groups + 1)], [n if g % 2 else 0 for g in range(groups + 1)], [2 ** 31 - 1] * (groups + 1)):
+        offsets = on_device(off)
+        y, dx = (torch.full((n + 64, w), MARK, dtype=TYPES[dtype], device="cuda") for w in (outer, inner))
+        u = torch.full((n + 64, rank), MARK, device="cuda")
+        dW, dA, dB = (torch.full((k + 1, *shape), MARK, device="cuda") for k, shape in ((groups, (outer, inner)), (slots, (rank, inner)), (slots, (outer, rank))))
+        sizes = [nb.grouped_workspace_bytes(layer, n) // 4, nb.adapter_workspace_bytes(adapted, n) // 4]
+        spaces = [torch.full((s + 256,), MARK, device="cuda") for s in sizes]
+        nb.grouped_fwd(layer, x, W, offsets, y[32:n + 32])
+        for given in (x, (q, e)):
+            nb.grouped_bwd(layer, given, W, offsets, dy, dx[32:n + 32], dW[:groups], spaces[0][:sizes[0]] if sizes[0] else None)
+        nb.adapter_fwd(adapted, x, W[0], A, B, scales, named, offsets, u[32:n + 32], y[32:n + 32])
+        nb.adapter_bwd(adapted, x, W[0], A, B, scales, named, offsets, u[32:n + 32], dy, dx[32:n + 32], dA[:slots], dB[:slots], spaces[1][:sizes[1]])
+        torch.cuda.synchronize()
+        for t in (y, dx, u):
+            assert torch.all(t[:32] == MARK) and torch.all(t[n + 32:] == MARK)
+        for t in (dW, dA, dB):
+            assert torch.all(t[-1] == MARK)
+        for t, s in zip(spaces, sizes):
+            assert torch.all(t[s:] == MARK)
+
+
 ADAPTERS = [  # n, groups, slots, inner, outer, rank, pad, before, behind
     (1, 1, 1, 1, 1, 1, 0, 0, 0), (3, 3, 2, 40, 20, 4, 0, 0, 0), (64, 64, 9, 200, 72, 16, 0, 0, 0), (61, 5, 3, 96, 136, 5, 3, 4, 3),
     (65, 65, 40, 64, 64, 8, 0, 0, 0), (500, 7, 7, 64, 64, 8, 0, 3, 9), (700, 3, 5, 136, 200, 64, 8, 0, 0), (1500, 100, 30, 300, 129, 33, 1, 1, 1),
