@@ -718,6 +718,7 @@ struct MatrixGradient {
     bool by_slot; const int32_t* slots; int n_slots;
 };
 int64_t matrix_gradient_bytes(const MatrixGradient& m);
+int check_matrix_gradient(const MatrixGradient& m);      // whether launch_matrix_gradient has numbers for all workgroups
 int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st);
 bool narrow_backward_fits(int dtype, int inner, int outer, int64_t groups, int64_t n, int64_t dy_stride, int64_t x_stride, bool packed);
 int64_t narrow_backward_bytes(int inner, int outer, int64_t groups);

@@ -767,6 +767,7 @@ int neus2_grouped_bwd(const neus2_layer* l, const void* x, const int8_t* xq, con
     // (the sums of dW alone come from the same kernel: the same bits with and without dx)
     if (narrow_backward_fits(l->dtype, l->in_dim, l->out_dim, l->groups, n, m.dy_stride, m.x_stride, xq != nullptr))
         return launch_narrow_backward(l->dtype, a, m, st);
+    NEUS2_TRY(check_matrix_gradient(m));
     if (dx && n > 0) NEUS2_TRY(launch_rows<true>(l->dtype, a, st));
     return launch_matrix_gradient(m, st);
 }

@@ -316,6 +316,17 @@ int64_t cut(const MatrixGradient& m, SumArgs& a, int outer_tile, int inner_tile)
     return chunk_count(group_count(m), m.groups.n, a.chunk) * a.outer_tiles * a.inner_tiles;
 }
 
+// whether its chunks, cut for the wide tiles, also take them
+bool wide_tiles_fit(const MatrixGradient& m) {
+    return wide_sums_fit(m) && rows_aligned(m.dtype, m.dy_stride) && m.dy_stride <= (1 << 20) &&
+           (m.xq || (rows_aligned(m.dtype, m.x_stride) && m.x_stride <= (1 << 20)));
+}
+
+int64_t sum_blocks(const MatrixGradient& m, SumArgs& a) {
+    a = sum_args(m, wide_sums_fit(m));
+    return wide_tiles_fit(m) ? cut(m, a, kWideOuter, kWideInner) : cut(m, a, tile_of(m.outer), tile_of(m.inner));
+}
+
 JoinArgs join_args(const MatrixGradient& m, const SumArgs& a, int64_t& blocks) {
     JoinArgs j = {};
     j.groups = m.groups;
@@ -366,17 +377,18 @@ int launch_adapter_gradients(const MatrixGradient& da, const MatrixGradient& db,
     return check_launch("adapter gradient sums");
 }
 
+int check_matrix_gradient(const MatrixGradient& m) {
+    SumArgs a;
+    return check_grid(sum_blocks(m, a));
+}
+
 int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
-    const bool wide = wide_sums_fit(m), f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
-    const bool aligned = rows_aligned(m.dtype, m.dy_stride) && m.dy_stride <= (1 << 20) &&
-                         (m.xq || (rows_aligned(m.dtype, m.x_stride) && m.x_stride <= (1 << 20)));
-    SumArgs a = sum_args(m, wide);
-    const int64_t blocks = cut(m, a, wide && aligned ? kWideOuter : tile_of(m.outer), wide && aligned ? kWideInner : tile_of(m.inner));
-    NEUS2_TRY(check_grid(blocks));
-    const unsigned grid = (unsigned)blocks;
+    const bool f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
+    SumArgs a;
+    const unsigned grid = (unsigned)sum_blocks(m, a);
     if (f32) {
         m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
-    } else if (wide && aligned) {
+    } else if (wide_tiles_fit(m)) {
         launch_wide_sums(m.dtype, m.xq != nullptr, a, grid, st);
     } else if (f16) {
         m.xq ? launch_sums<Native, Packed<true>, true>(a, grid, st) : launch_sums<Native, Native, true>(a, grid, st);

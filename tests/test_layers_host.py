@@ -220,3 +220,9 @@ def test_the_8_bit_form_is_half_a_step_away_at_most():
     assert np.array_equal(mask, x > 0) and not q[:, 70:].any()
     words = lo.mask_words(mask).view(np.uint32)
     assert np.array_equal((words[:, 2] >> 5) & 1, mask[:, 69].astype(np.uint32)) and not (words[:, 2] >> 6).any()
+
+
+def test_a_refused_backward_call_has_launched_nothing():
+    """More workgroups for dW than there are numbers: refused before dx is written, not after (without a GPU that launch would fail first)."""
+    l = layer(dtype="bf16", groups=1 << 16, out_dim=65536, in_dim=65536)
+    assert grouped_bwd(l, n=1 << 16) == -2 and b"workgroups" in nb.lib().neus2_last_error()
