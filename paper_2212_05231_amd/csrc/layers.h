@@ -461,6 +461,7 @@ struct RowsArgs {
     const int32_t* slots; int n_slots;
     const float* u; const void* bank; int rank;
     int col_tiles;
+    int first_block;                 // workgroups launched before (launch_blocks)
 };
 
 // The number of bf16 terms an adapter's fp32 u and its bank matrix take in y += bank u.
@@ -661,6 +662,7 @@ struct SumArgs {
     int partials;
     int by_slot;
     int outer_tiles, inner_tiles;
+    int first_block;
 };
 
 // Where a chunk's sums belong, and whether they are added to what is there; NULL: nowhere.
@@ -700,7 +702,7 @@ __device__ __forceinline__ void store_sums(const SumArgs& a, const RowTile& t, i
 }
 
 constexpr int kWideOuter = 256, kWideInner = 256;       // their tiles
-void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st);
+void launch_wide_sums(int dtype, bool packed, const SumArgs& a, int64_t blocks, hipStream_t st);
 int launch_wide_rows(int dtype, bool backward, const RowsArgs& a, hipStream_t st);      // 16-bit types, whole lines of the contraction
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------
@@ -739,9 +741,15 @@ inline int64_t row_tiles(const RowGroups& g, int rows) {
     return tiles < g.n ? tiles : g.n;
 }
 
-inline int check_grid(int64_t blocks) {
-    if (blocks > 0x7fffffff) return fail(NEUS2_ERR_SHAPE, "%lld workgroups: too many rows for so many outputs", (long long)blocks);
-    return NEUS2_OK;
+// A launch has fewer than 2^32 threads in a dimension: more workgroups than that go in several launches, go(grid, first) each, and a
+// kernel's block number is first + blockIdx.x.  Numbers stay below 2^31: 2^28 rows in tiles of 128 beside 2^16 groups and 2^16 outputs in
+// tiles of 128 are 2^30.1; tiles of 64 and 16 are taken for few tiles or rows only; the sums of matrices check theirs.
+constexpr int64_t kMostThreads = 0xffffffffll;
+
+template <class Go>
+inline void launch_blocks(int64_t blocks, int threads, const Go& go) {
+    const int64_t most = kMostThreads / threads;
+    for (int64_t first = 0; first < blocks; first += most) go((unsigned)(blocks - first < most ? blocks - first : most), (int)first);
 }
 
 }  // namespace neus2

@@ -28,8 +28,8 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WC, wc = wave % WC;
-    const int col0 = (int)(blockIdx.x % a.col_tiles) * COLS;
-    const RowTile t = locate(a.groups, ROWS, 0, (int)(blockIdx.x / a.col_tiles), lane);
+    const int block = a.first_block + (int)blockIdx.x, col0 = block % a.col_tiles * COLS;
+    const RowTile t = locate(a.groups, ROWS, 0, block / a.col_tiles, lane);
     if (t.group < 0) return;
 
     typename Factor::Pointer data, matrix;
@@ -192,6 +192,7 @@ struct FewArgs {
     int relu;
     const int32_t* segments; int n_segments; const int32_t* slots; int n_slots; const float* u; const void* bank; int rank;
     int col_tiles;
+    int first_block;
 };
 
 constexpr int kFewWaves = 8;
@@ -209,8 +210,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(FewArgs a) {
     __shared__ int row_slot[16];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col0 = (int)(blockIdx.x % a.col_tiles) * 16;
-    const RowTile t = locate(a.groups, 16, 0, (int)(blockIdx.x / a.col_tiles), lane);
+    const int block = a.first_block + (int)blockIdx.x, col0 = block % a.col_tiles * 16;
+    const RowTile t = locate(a.groups, 16, 0, block / a.col_tiles, lane);
     if (t.group < 0) return;
 
     const int i = lane & 15, quarter = lane >> 4;
@@ -306,6 +307,7 @@ struct LowRankArgs {
     int steps, rank;
     const int32_t* slots; int n_slots; const float* scales;
     float* u;
+    int first_block;
 };
 
 template <int DT, bool DOWN, bool SPLIT, int BLOCKS>
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(512, SPLIT ? 4 : 2) void low_rank_kernel(LowRankArg
     __shared__ float part[SPLIT ? kWaves : 1][SPLIT ? BLOCKS * 16 : 1][33];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, (int)blockIdx.x, lane);
+    RowTile t = locate(a.groups, SPLIT ? 32 : 32 * kWaves, 0, a.first_block + (int)blockIdx.x, lane);
     if (t.group < 0) return;
     if (!SPLIT) {
         t.lo += 32 * wave;
@@ -533,9 +535,18 @@ __global__ __launch_bounds__(256) void unpack_kernel(const int8_t* __restrict__ 
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------------------
+template <int DT, bool BACKWARD, bool ADAPT, bool ONCE, int ROWS, int COLS, int WR, int WC>
+void launch_tiles(RowsArgs a, hipStream_t st) {
+    constexpr int kDepth = DT == kTypeF32 ? 32 : 64, kBufs = DT == kTypeF32 ? 1 : 2, kThreads = 64 * WR * WC;
+    a.col_tiles = (a.cols + COLS - 1) / COLS;
+    launch_blocks(row_tiles(a.groups, ROWS) * a.col_tiles, kThreads, [&](unsigned grid, int first) {
+        a.first_block = first;
+        rows_kernel<DT, BACKWARD, ADAPT, ONCE, ROWS, COLS, WR, WC, kDepth, kBufs><<<grid, kThreads, 0, st>>>(a);
+    });
+}
+
 template <int DT, bool BACKWARD, bool ADAPT, bool ONCE>
-int launch_rows(RowsArgs a, hipStream_t st) {
-    constexpr int kDepth = DT == kTypeF32 ? 32 : 64, kBufs = DT == kTypeF32 ? 1 : 2;
+int launch_rows(const RowsArgs& a, hipStream_t st) {
     if (!ADAPT && a.cols <= 64 && a.steps <= 64 && a.x_whole) {
         const int64_t tiles = row_tiles(a.groups, kNarrowRows);
         const unsigned grid = (unsigned)persistent_blocks((const void*)narrow_rows_kernel<DT, BACKWARD, ONCE>, 256, tiles);
@@ -543,16 +554,11 @@ int launch_rows(RowsArgs a, hipStream_t st) {
     } else if (row_tiles(a.groups, 128) * ((a.cols + 127) / 128) < 2 * compute_units()) {
         // too few tiles of 128 x 128 to hide each other's waits (2048 to 2048: bf16 2^9 rows 24 us against 33, 2^11 rows 37 against 42, 2^12
         // rows 71 against 48; fp32 2^11 rows 126 against 138, 2^12 rows 255 against 185)
-        a.col_tiles = (a.cols + 63) / 64;
-        NEUS2_TRY(check_grid(row_tiles(a.groups, 64) * a.col_tiles));
-        rows_kernel<DT, BACKWARD, ADAPT, ONCE, 64, 64, 2, 1, kDepth, kBufs><<<dim3((unsigned)(row_tiles(a.groups, 64) * a.col_tiles)), 128, 0, st>>>(a);
+        launch_tiles<DT, BACKWARD, ADAPT, ONCE, 64, 64, 2, 1>(a, st);
     } else if (a.cols > 64) {
-        a.col_tiles = (a.cols + 127) / 128;
-        NEUS2_TRY(check_grid(row_tiles(a.groups, 128) * a.col_tiles));
-        rows_kernel<DT, BACKWARD, ADAPT, ONCE, 128, 128, 2, 2, kDepth, kBufs><<<dim3((unsigned)(row_tiles(a.groups, 128) * a.col_tiles)), 256, 0, st>>>(a);
+        launch_tiles<DT, BACKWARD, ADAPT, ONCE, 128, 128, 2, 2>(a, st);
     } else {
-        a.col_tiles = 1;
-        rows_kernel<DT, BACKWARD, ADAPT, ONCE, 128, 64, 4, 1, kDepth, kBufs><<<dim3((unsigned)row_tiles(a.groups, 128)), 256, 0, st>>>(a);
+        launch_tiles<DT, BACKWARD, ADAPT, ONCE, 128, 64, 4, 1>(a, st);
     }
     return check_launch(BACKWARD ? "layer backward" : "layer forward");
 }
@@ -584,11 +590,12 @@ int launch_rows(int dtype, const RowsArgs& args, hipStream_t st) {
 
 int launch_few(int dtype, FewArgs a, hipStream_t st) {
     a.col_tiles = (a.cols + 15) / 16;
-    const int64_t blocks = row_tiles(a.groups, 16) * a.col_tiles;
-    NEUS2_TRY(check_grid(blocks));
-    if (dtype == kTypeF32) few_rows_kernel<kTypeF32><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
-    else if (dtype == kTypeF16) few_rows_kernel<kTypeF16><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
-    else few_rows_kernel<kTypeBF16><<<(unsigned)blocks, 64 * kFewWaves, 0, st>>>(a);
+    launch_blocks(row_tiles(a.groups, 16) * a.col_tiles, 64 * kFewWaves, [&](unsigned grid, int first) {
+        a.first_block = first;
+        if (dtype == kTypeF32) few_rows_kernel<kTypeF32><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else if (dtype == kTypeF16) few_rows_kernel<kTypeF16><<<grid, 64 * kFewWaves, 0, st>>>(a);
+        else few_rows_kernel<kTypeBF16><<<grid, 64 * kFewWaves, 0, st>>>(a);
+    });
     return check_launch("layer, few rows");
 }
 
@@ -611,15 +618,15 @@ RowGroups make_groups(const int32_t* offsets, int groups, int64_t n, bool whole)
 }
 
 template <int DT, bool DOWN>
-int launch_low_rank(const LowRankArgs& a, hipStream_t st) {
+int launch_low_rank(LowRankArgs a, hipStream_t st) {
     // contractions of up to 256 steps are not worth sharing: every wave has rows of its own
     const bool split = a.steps > 256;
-    const int64_t blocks = row_tiles(a.groups, split ? 32 : 256);
-    NEUS2_TRY(check_grid(blocks));
-    const unsigned grid = (unsigned)blocks;
-    if (a.rank > 32) split ? low_rank_kernel<DT, DOWN, true, 4><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 4><<<grid, 512, 0, st>>>(a);
-    else if (a.rank > 16) split ? low_rank_kernel<DT, DOWN, true, 2><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 2><<<grid, 512, 0, st>>>(a);
-    else split ? low_rank_kernel<DT, DOWN, true, 1><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 1><<<grid, 512, 0, st>>>(a);
+    launch_blocks(row_tiles(a.groups, split ? 32 : 256), 512, [&](unsigned grid, int first) {
+        a.first_block = first;
+        if (a.rank > 32) split ? low_rank_kernel<DT, DOWN, true, 4><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 4><<<grid, 512, 0, st>>>(a);
+        else if (a.rank > 16) split ? low_rank_kernel<DT, DOWN, true, 2><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 2><<<grid, 512, 0, st>>>(a);
+        else split ? low_rank_kernel<DT, DOWN, true, 1><<<grid, 512, 0, st>>>(a) : low_rank_kernel<DT, DOWN, false, 1><<<grid, 512, 0, st>>>(a);
+    });
     return check_launch("adapter");
 }
 

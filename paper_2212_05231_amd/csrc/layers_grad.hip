@@ -102,7 +102,7 @@ __device__ __forceinline__ void matrix_sums(const SumArgs& a, int block, unsigne
 template <class Left, class Right, bool HALF, int OUTER, int INNER>
 __global__ __launch_bounds__(256) void matrix_sums_kernel(SumArgs a) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[SumShape<Left, Right, OUTER, INNER>::kBytes];
-    matrix_sums<Left, Right, HALF, OUTER, INNER>(a, (int)blockIdx.x, lds);
+    matrix_sums<Left, Right, HALF, OUTER, INNER>(a, a.first_block + (int)blockIdx.x, lds);
 }
 
 // Both narrow matrices of adapters, dA (v x^T) and dB (dy u^T), in one launch: each alone is a row of waits (8192 rows, 2048 wide, rank
@@ -112,8 +112,9 @@ __global__ __launch_bounds__(256) void adapter_sums_kernel(SumArgs a, SumArgs b,
     typedef SumShape<V, X, 64, WIDE> A;
     typedef SumShape<Dy, U, WIDE, 64> B;
     __shared__ __attribute__((aligned(16))) unsigned char lds[A::kBytes > B::kBytes ? A::kBytes : B::kBytes];
-    if ((int)blockIdx.x < blocks_a) matrix_sums<V, X, false, 64, WIDE>(a, (int)blockIdx.x, lds);
-    else matrix_sums<Dy, U, false, WIDE, 64>(b, (int)blockIdx.x - blocks_a, lds);
+    const int block = a.first_block + (int)blockIdx.x;
+    if (block < blocks_a) matrix_sums<V, X, false, 64, WIDE>(a, block, lds);
+    else matrix_sums<Dy, U, false, WIDE, 64>(b, block - blocks_a, lds);
 }
 
 // Adds the chunks' sums.  A workgroup has 256 elements of one matrix; each of its four waves adds every fourth chunk in the order of
@@ -258,12 +259,15 @@ int64_t partial_count(int groups, int64_t n, int64_t splits, bool by_slot) {
 }
 
 template <class Left, class Right, bool HALF>
-void launch_sums(const SumArgs& a, unsigned grid, hipStream_t st) {
+void launch_sums(SumArgs a, int64_t blocks, hipStream_t st) {
     const bool o = a.outer > 64, i = a.inner > 64;
-    if (o && i) matrix_sums_kernel<Left, Right, HALF, 128, 128><<<grid, 256, 0, st>>>(a);
-    else if (o) matrix_sums_kernel<Left, Right, HALF, 128, 64><<<grid, 256, 0, st>>>(a);
-    else if (i) matrix_sums_kernel<Left, Right, HALF, 64, 128><<<grid, 256, 0, st>>>(a);
-    else matrix_sums_kernel<Left, Right, HALF, 64, 64><<<grid, 256, 0, st>>>(a);
+    launch_blocks(blocks, 256, [&](unsigned grid, int first) {
+        a.first_block = first;
+        if (o && i) matrix_sums_kernel<Left, Right, HALF, 128, 128><<<grid, 256, 0, st>>>(a);
+        else if (o) matrix_sums_kernel<Left, Right, HALF, 128, 64><<<grid, 256, 0, st>>>(a);
+        else if (i) matrix_sums_kernel<Left, Right, HALF, 64, 128><<<grid, 256, 0, st>>>(a);
+        else matrix_sums_kernel<Left, Right, HALF, 64, 64><<<grid, 256, 0, st>>>(a);
+    });
 }
 
 }  // namespace
@@ -347,9 +351,12 @@ JoinArgs join_args(const MatrixGradient& m, const SumArgs& a, int64_t& blocks) {
 }
 
 template <class V, class X, class Dy, class U>
-void launch_adapter_sums(const SumArgs& a, const SumArgs& b, bool wide, int64_t blocks_a, int64_t blocks, hipStream_t st) {
-    if (wide) adapter_sums_kernel<V, X, Dy, U, 128><<<(unsigned)blocks, 256, 0, st>>>(a, b, (int)blocks_a);
-    else adapter_sums_kernel<V, X, Dy, U, 64><<<(unsigned)blocks, 256, 0, st>>>(a, b, (int)blocks_a);
+void launch_adapter_sums(SumArgs a, const SumArgs& b, bool wide, int64_t blocks_a, int64_t blocks, hipStream_t st) {
+    launch_blocks(blocks, 256, [&](unsigned grid, int first) {
+        a.first_block = first;
+        if (wide) adapter_sums_kernel<V, X, Dy, U, 128><<<grid, 256, 0, st>>>(a, b, (int)blocks_a);
+        else adapter_sums_kernel<V, X, Dy, U, 64><<<grid, 256, 0, st>>>(a, b, (int)blocks_a);
+    });
 }
 
 }  // namespace
@@ -358,7 +365,6 @@ int launch_adapter_gradients(const MatrixGradient& da, const MatrixGradient& db,
     SumArgs a = sum_args(da, false), b = sum_args(db, false);
     const bool wide = da.inner > 64 || db.outer > 64;
     const int64_t blocks_a = cut(da, a, 64, wide ? 128 : 64), blocks = blocks_a + cut(db, b, wide ? 128 : 64, 64);
-    NEUS2_TRY(check_grid(blocks));
     if (da.dtype == kTypeF32) {
         if (da.xq) launch_adapter_sums<Wide<3>, Packed<false>, Wide<3>, Wide<3>>(a, b, wide, blocks_a, blocks, st);
         else launch_adapter_sums<Wide<3>, Wide<3>, Wide<3>, Wide<3>>(a, b, wide, blocks_a, blocks, st);
@@ -372,34 +378,35 @@ int launch_adapter_gradients(const MatrixGradient& da, const MatrixGradient& db,
     NEUS2_TRY(check_launch("adapter gradients"));
     int64_t joins_a, joins_b;
     const JoinArgs ja = join_args(da, a, joins_a), jb = join_args(db, b, joins_b);
-    NEUS2_TRY(check_grid(joins_a + joins_b));
     join_sums_kernel<<<(unsigned)(joins_a + joins_b), 256, 0, st>>>(ja, jb, (int)joins_a);
     return check_launch("adapter gradient sums");
 }
 
 int check_matrix_gradient(const MatrixGradient& m) {
     SumArgs a;
-    return check_grid(sum_blocks(m, a));
+    const int64_t blocks = sum_blocks(m, a);
+    if (blocks > 0x7fffffff)
+        return fail(NEUS2_ERR_SHAPE, "%lld workgroups for dW: too many groups for so large matrices", (long long)blocks);
+    return NEUS2_OK;
 }
 
 int launch_matrix_gradient(const MatrixGradient& m, hipStream_t st) {
     const bool f32 = m.dtype == kTypeF32, f16 = m.dtype == kTypeF16;
     SumArgs a;
-    const unsigned grid = (unsigned)sum_blocks(m, a);
+    const int64_t blocks = sum_blocks(m, a);
     if (f32) {
-        m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, grid, st) : launch_sums<Wide<3>, Wide<3>, false>(a, grid, st);
+        m.xq ? launch_sums<Wide<3>, Packed<false>, false>(a, blocks, st) : launch_sums<Wide<3>, Wide<3>, false>(a, blocks, st);
     } else if (wide_tiles_fit(m)) {
-        launch_wide_sums(m.dtype, m.xq != nullptr, a, grid, st);
+        launch_wide_sums(m.dtype, m.xq != nullptr, a, blocks, st);
     } else if (f16) {
-        m.xq ? launch_sums<Native, Packed<true>, true>(a, grid, st) : launch_sums<Native, Native, true>(a, grid, st);
+        m.xq ? launch_sums<Native, Packed<true>, true>(a, blocks, st) : launch_sums<Native, Native, true>(a, blocks, st);
     } else {
-        m.xq ? launch_sums<Native, Packed<false>, false>(a, grid, st) : launch_sums<Native, Native, false>(a, grid, st);
+        m.xq ? launch_sums<Native, Packed<false>, false>(a, blocks, st) : launch_sums<Native, Native, false>(a, blocks, st);
     }
     NEUS2_TRY(check_launch("matrix gradient"));
     if (a.partials == 0) return NEUS2_OK;                               // every group was one chunk
     int64_t joins;
     const JoinArgs j = join_args(m, a, joins);
-    NEUS2_TRY(check_grid(joins));
     join_sums_kernel<<<(unsigned)joins, 256, 0, st>>>(j, j, (int)joins);
     return check_launch("matrix gradient sums");
 }

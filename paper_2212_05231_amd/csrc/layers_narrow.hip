@@ -277,7 +277,6 @@ int launch_narrow_backward(int dtype, const RowsArgs& rows, const MatrixGradient
     NEUS2_TRY(check_launch("narrow layer backward"));
     const int size = m.inner * m.outer, blocks = (size + 255) / 256;
     const int64_t joins = (int64_t)(m.groups.offsets ? m.groups.groups : 1) * blocks;
-    NEUS2_TRY(check_grid(joins));
     run_join_kernel<<<(unsigned)joins, 256, 0, st>>>(m.groups, runs, size, blocks, m.partial, m.out, m.accumulate);
     return check_launch("narrow layer backward sums");
 }

@@ -247,8 +247,8 @@ __global__ __launch_bounds__(kThreads, 2) void wide_sums_kernel(SumArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wo = wave >> 2, wi = wave & 3;
     const int tiles = a.outer_tiles * a.inner_tiles;
-    const int tile = (int)(blockIdx.x % tiles), outer0 = tile / a.inner_tiles * kLeft, inner0 = tile % a.inner_tiles * kRight;
-    const RowTile t = locate<true>(a.groups, a.chunk, 1, (int)(blockIdx.x / tiles), lane);
+    const int block = a.first_block + (int)blockIdx.x, tile = block % tiles, outer0 = tile / a.inner_tiles * kLeft, inner0 = tile % a.inner_tiles * kRight;
+    const RowTile t = locate<true>(a.groups, a.chunk, 1, block / tiles, lane);
     if (t.group < 0) return;
 
     WideTile<false, kLeft> lt;
@@ -306,8 +306,14 @@ unsigned wide_blocks(int64_t pieces) {
 
 }  // namespace
 
-void launch_wide_sums(int dtype, bool packed, const SumArgs& a, unsigned grid, hipStream_t st) {
-    auto go = [&](auto* plain, auto* once) { (a.once ? once : plain)<<<grid, kThreads, 0, st>>>(a); };
+void launch_wide_sums(int dtype, bool packed, const SumArgs& args, int64_t blocks, hipStream_t st) {
+    SumArgs a = args;
+    auto go = [&](auto* plain, auto* once) {
+        launch_blocks(blocks, kThreads, [&](unsigned grid, int first) {
+            a.first_block = first;
+            (a.once ? once : plain)<<<grid, kThreads, 0, st>>>(a);
+        });
+    };
     if (dtype == kTypeF16) {
         if (packed) go(wide_sums_kernel<kTypeF16, true, false>, wide_sums_kernel<kTypeF16, true, true>);
         else go(wide_sums_kernel<kTypeF16, false, false>, wide_sums_kernel<kTypeF16, false, true>);
@@ -321,7 +327,7 @@ int launch_wide_rows(int dtype, bool backward, const RowsArgs& args, hipStream_t
     RowsArgs a = args;
     a.col_tiles = (a.cols + kLeft - 1) / kLeft;
     const int64_t pieces = row_tiles(a.groups, kRight) * a.col_tiles;
-    NEUS2_TRY(check_grid(pieces));
+    // (one launch: beside a shared matrix, whose rows are one group, its limit of 2^23 tiles is 550 GB of outputs)
     const unsigned grid = a.rank > 0 ? (unsigned)((pieces + kXcds - 1) / kXcds * kXcds) : wide_blocks(pieces);
     if (dtype == kTypeF16) backward ? launch<kTypeF16, true>(a, grid, st) : launch<kTypeF16, false>(a, grid, st);
     else backward ? launch<kTypeBF16, true>(a, grid, st) : launch<kTypeBF16, false>(a, grid, st);
