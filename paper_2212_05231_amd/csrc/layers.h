@@ -3,9 +3,8 @@
 //
 // Types.  bf16 and fp16 factors go to the matrix cores as they are, one instruction per k-step, accumulated in fp32.  fp32
 // factors are sums of bf16 terms as in mfma_tile.h: three terms and six products, as accurate as an fp32 product.  Where a
-// factor kept in fp32 (an adapter's u or v) meets one of 16 bits, an fp16 one is two bf16 terms (8 + 8 >= 11 bits: exact), so
-// that small gradients do not fall out of fp16's range; the fp32 one takes three terms where the result is fp32 (dA, dB), and
-// two (2^-17 relative) where it is rounded to 16 bits (y, dx).  An infinite fp32 factor makes its products NaN (inf - inf in the split).
+// factor kept in fp32 (an adapter's u or v) meets one of 16 bits, the fp32 one takes three terms there too and an fp16 one two (8 + 8 >=
+// 11 bits: exact), so that small gradients do not fall out of fp16's range.  An infinite fp32 factor makes its products NaN (inf - inf in the split).
 #pragma once
 
 #include "common.h"
@@ -464,9 +463,10 @@ struct RowsArgs {
     int first_block;                 // workgroups launched before (launch_blocks)
 };
 
-// The number of bf16 terms an adapter's fp32 u and its bank matrix take in y += bank u.
+// The number of bf16 terms an adapter's fp32 u and its bank matrix take in y += bank u.  Two for u would be enough for a sum that is
+// rounded to 16 bits, but not where W x and bank u cancel: there the difference is what they leave out.
 template <int DT> struct AdapterTerms {
-    static constexpr int kU = DT == kTypeF32 ? 3 : 2;
+    static constexpr int kU = 3;
     static constexpr int kBank = DT == kTypeF32 ? 3 : DT == kTypeF16 ? 2 : 1;
 };
 

@@ -45,3 +45,80 @@ def test_gradients_of_more_workgroups_than_a_launch_has():
         part = slice(g, g + 1024)
         assert torch.equal(dx[part], (W[part, 0].float() * dy[part].float()).bfloat16()), g
         assert torch.equal(dW[part, 0], x[part].float() * dy[part].float()), g
+
+
+# ---- what is left where large parts cancel ---------------------------------------------------------------------------------------------
+
+def three_terms(v):
+    """fp32 v as its bf16 rounding, that of the rest, and the rest of both."""
+    hi = v.bfloat16().float()
+    mid = (v - hi).bfloat16().float()
+    return hi, mid, v - hi - mid
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,inner,outer", [(16, 64, 64), (300, 64, 64), (66000, 64, 64), (17000, 72, 520), (17000, 520, 72), (8400, 64, 1024), (8400, 1024, 64)])
+def test_adapters_add_all_of_u_and_v(n, inner, outer, dtype):
+    """Rows in which W x (backward: W^T dy) takes away the first two bf16 terms of B u (A^T v): what comes out is the third one, of at most
+    7 bits.  u and v hold all 24 bits of a scale; every product and partial sum is a multiple of 2^-23 below 2: nothing is rounded."""
+    gen = torch.Generator().manual_seed(n + outer)
+    slots, rank, groups = 8, 8, 20
+    s = 1.0 + torch.rand(slots, generator=gen) * 0.9
+    hi, mid, rest = three_terms(s)
+    assert (rest != 0).sum() >= 6 and rest.abs().max() <= 2.0 ** -17
+    named = [g % slots for g in range(groups)]
+    off = split_rows(n, groups, gen)
+    scales, slot_of_row = s.cuda(), torch.zeros(n, dtype=torch.long)
+    for g in range(groups):
+        slot_of_row[off[g]:off[g + 1]] = named[g]
+    ones = lambda width: torch.zeros(n, width).scatter_(1, 2 * slot_of_row[:, None] + torch.arange(2), 1.0).to(TYPES[dtype]).cuda()
+    part = torch.stack((-hi, -mid), 1).reshape(16)                                     # what the shared matrix takes away
+    A, B = torch.zeros(slots, rank, inner), torch.zeros(slots, outer, rank)
+    layer = nb.make_layer(dtype, groups, inner, outer, rank=rank, adapters=slots)
+    move = lambda t: t.to(TYPES[dtype]).cuda()
+    # forward: u = s A x = s
+    W = torch.zeros(outer, inner)
+    W[:, :16] = part
+    A[torch.arange(slots), 0, 2 * torch.arange(slots)] = 1.0
+    B[:, :, 0] = 1.0
+    assert torch.equal(move(W).float().cpu(), W)
+    y, u = empty(n, outer, outer, dtype), torch.full((n, rank), MARK, device="cuda")
+    nb.adapter_fwd(layer, ones(inner), move(W), move(A), move(B), scales, on_device(named), on_device(off), u, y)
+    assert torch.equal(u[:, 0].cpu(), s[slot_of_row])
+    assert torch.equal(y.float().cpu(), rest[slot_of_row][:, None].expand(n, outer))
+    # backward: v = s B^T dy = s
+    W, A, B = torch.zeros(outer, inner), torch.zeros_like(A), torch.zeros_like(B)
+    W[:16] = part[:, None]
+    B[torch.arange(slots), 2 * torch.arange(slots), 0] = 1.0
+    A[:, 0, :] = 1.0
+    dx = empty(n, inner, inner, dtype)
+    workspace = torch.zeros(nb.adapter_workspace_bytes(layer, n) // 4, device="cuda")
+    nb.adapter_bwd(layer, None, move(W), move(A), move(B), scales, on_device(named), on_device(off), None, ones(outer), dx, None, None, workspace)
+    assert torch.equal(dx.float().cpu(), rest[slot_of_row][:, None].expand(n, inner))
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,groups,slots,inner,outer,rank", [(700, 5, 3, 136, 200, 64), (1500, 100, 30, 300, 129, 33), (900, 9, 4, 256, 64, 8)])
+def test_gradients_of_adapters_take_three_terms(n, groups, slots, inner, outer, rank, dtype, packed, accumulate):
+    """dA and dB of 16-bit layers are fp32 results of fp32 u and v: as near as those of an fp32 layer (two terms: 2^-17 a product)."""
+    gen = torch.Generator().manual_seed(n)
+    off, named = split_rows(n, groups, gen), torch.randint(0, slots, (groups,), generator=gen).tolist()
+    x, dy = rows(n, inner, inner, dtype, gen), rows(n, outer, outer, dtype, gen, 0.01)
+    W = (torch.randn(outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    A = (torch.randn(slots, rank, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    B = (torch.randn(slots, outer, rank, generator=gen) * rank ** -0.5).to(TYPES[dtype]).cuda()
+    scales, u = (torch.rand(slots, generator=gen) + 0.5).cuda(), torch.randn(n, rank, generator=gen).cuda()
+    q8, e8, _ = lo.pack8(f64(x), dtype)
+    x64 = lo.unpack8(q8, e8, inner) if packed else f64(x)
+    given = (torch.as_tensor(q8).cuda(), torch.as_tensor(e8).cuda()) if packed else x
+    args = (f64(W), f64(A), f64(B), f64(scales), named, off)
+    _, want_dA, want_dB = lo.adapter_backward(x64, *args, f64(u), f64(dy))
+    layer = nb.make_layer(dtype, groups, inner, outer, rank=rank, adapters=slots, accumulate=bool(accumulate))
+    dA, dB = (torch.randn(w.shape, generator=gen).cuda() * float(np.abs(w).mean()) for w in (want_dA, want_dB))
+    start = [f64(t) if accumulate else 0.0 for t in (dA, dB)]
+    workspace = torch.zeros(nb.adapter_workspace_bytes(layer, n) // 4, device="cuda")
+    nb.adapter_bwd(layer, given, None, A, B, scales, on_device(named), on_device(off), u, dy, None, dA, dB, workspace)
+    for got, want, s in zip((dA, dB), (want_dA, want_dB), start):
+        assert np.linalg.norm(f64(got) - (want + s)) <= 2e-6 * np.linalg.norm(want)
