@@ -448,8 +448,9 @@ int neus2_march_rays(int log2_res, const uint32_t* bitfield, const float* origin
  *   group are neither read nor written.  offsets may be NULL with one group: all n rows.  Offsets are
  *   cut to 0..n on the device: wrong ones give wrong results, never an access outside the arrays.
  * Types: x, y, dx, dy, W, A, B have the layer's dtype; sums are fp32 (fp32 factors: three bf16 terms,
- *   as accurate as an fp32 product); gradients of matrices, u and scales are fp32.  An infinite fp32
- *   factor gives NaN in the results it enters.
+ *   as accurate as an fp32 product); gradients of matrices, u and scales are fp32.  An infinite
+ *   factor of an fp32 layer, u, v or an adapter's matrix makes the sums it enters NaN, or infinite as
+ *   in the formula; 16-bit products are the formula's.  It reaches no other row, output or adapter.
  * Row strides: x_stride, y_stride count values from one row to the next (0: in_dim, out_dim); dx has
  *   x's, dy has y's.  Any stride works, multiples of 16 bytes are the fast ones.
  * accumulate: matrix gradients are ADDED into (1) or overwritten (0: groups without rows get zeros).

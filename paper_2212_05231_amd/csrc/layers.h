@@ -4,7 +4,7 @@
 // Types.  bf16 and fp16 factors go to the matrix cores as they are, one instruction per k-step, accumulated in fp32.  fp32
 // factors are sums of bf16 terms as in mfma_tile.h: three terms and six products, as accurate as an fp32 product.  Where a
 // factor kept in fp32 (an adapter's u or v) meets one of 16 bits, the fp32 one takes three terms there too and an fp16 one two (8 + 8 >=
-// 11 bits: exact), so that small gradients do not fall out of fp16's range.  An infinite fp32 factor makes its products NaN (inf - inf in the split).
+// 11 bits: exact), so that small gradients do not fall out of fp16's range.  An infinite factor that is split makes its products NaN (inf - inf).
 #pragma once
 
 #include "common.h"
@@ -173,8 +173,12 @@ __device__ __forceinline__ int segment_of(const int32_t* __restrict__ offsets, i
 // A factor is read eight consecutive values at a time (a unit) and becomes kTerms words of eight 16-bit values.
 __device__ __forceinline__ u32x4 zero4() { return u32x4{0u, 0u, 0u, 0u}; }
 
-template <int TERMS>
+// LARGE: values above bf16's largest number (0.4 % below fp32's) take that as their first term, which rounding would make infinite; what is
+// left comes with the others.  (So do infinities and NaN, of which infinities and NaN are left.)
+template <int TERMS, bool LARGE = true>
 __device__ __forceinline__ void split8(f32x8 v, u32x4 (&out)[TERMS]) {
+    typedef int16_t s2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u2 __attribute__((ext_vector_type(2)));
     typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
     typedef float f2 __attribute__((ext_vector_type(2)));
 #pragma unroll
@@ -182,7 +186,11 @@ __device__ __forceinline__ void split8(f32x8 v, u32x4 (&out)[TERMS]) {
         float x0 = v[2 * p], x1 = v[2 * p + 1];
 #pragma unroll
         for (int term = 0; term < TERMS; ++term) {
-            const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x0, x1}, bf2));
+            uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x0, x1}, bf2));
+            if (LARGE && term == 0) {
+                w = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(s2, w), s2{0x7f7f, 0x7f7f}));        // positive ones
+                w = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u2, w), u2{0xff7f, 0xff7f}));        // negative ones
+            }
             out[term][p] = w;
             x0 -= __builtin_bit_cast(float, w << 16);
             x1 -= __builtin_bit_cast(float, w & 0xffff0000u);
@@ -275,7 +283,7 @@ struct HalfPair {
     __device__ static __forceinline__ Raw fetch(const Window& w, int row, int col, bool in) { return Native::fetch(w, row, col, in); }
     __device__ static __forceinline__ Raw load(const Pointer& f, int64_t row, int col, int valid) { return Native::load(f, row, col, valid); }
     __device__ static __forceinline__ void terms(const Raw& r, u32x4 (&out)[2]) {
-        split8<2>(__builtin_convertvector(__builtin_bit_cast(h8, r.v), f32x8), out);
+        split8<2, false>(__builtin_convertvector(__builtin_bit_cast(h8, r.v), f32x8), out);
     }
 };
 
@@ -522,7 +530,7 @@ __device__ __forceinline__ void bank_terms(const BankRaw<DT>& raw, u32x4 (&out)[
     if constexpr (DT == kTypeF32) {
         split8<3>(__builtin_shufflevector(__builtin_bit_cast(v4f, raw.v[0]), __builtin_bit_cast(v4f, raw.v[1]), 0, 1, 2, 3, 4, 5, 6, 7), out);
     } else if constexpr (DT == kTypeF16) {
-        split8<2>(__builtin_convertvector(__builtin_bit_cast(h8, raw.v[0]), f32x8), out);
+        split8<2, false>(__builtin_convertvector(__builtin_bit_cast(h8, raw.v[0]), f32x8), out);
     } else {
         out[0] = raw.v[0];
     }

@@ -316,7 +316,7 @@ __global__ __launch_bounds__(512, SPLIT ? 4 : 2) void low_rank_kernel(LowRankArg
     typedef std::conditional_t<DT == kTypeF32, Wide<3>, Native> Factor;
     constexpr int kTerms = Factor::kTerms;
     // k-steps (of 32) whose operands are in flight together: as many as leave registers for a second workgroup on the compute unit
-    constexpr int kAhead = DT == kTypeF32 ? (BLOCKS > 2 ? 1 : 2) : BLOCKS > 2 ? (DOWN ? 1 : 2) : DOWN && BLOCKS > 1 ? 2 : 4;
+    constexpr int kAhead = DT == kTypeF32 ? (BLOCKS > (DOWN ? 1 : 2) ? 1 : 2) : BLOCKS > 2 ? (DOWN ? 1 : 2) : DOWN && BLOCKS > 1 ? 2 : 4;
     constexpr bool kHalf = DT == kTypeF16;
     constexpr int kWaves = 8;
     __shared__ float part[SPLIT ? kWaves : 1][SPLIT ? BLOCKS * 16 : 1][33];

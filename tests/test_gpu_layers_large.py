@@ -122,3 +122,85 @@ def test_gradients_of_adapters_take_three_terms(n, groups, slots, inner, outer, 
     nb.adapter_bwd(layer, given, None, A, B, scales, on_device(named), on_device(off), u, dy, None, dA, dB, workspace)
     for got, want, s in zip((dA, dB), (want_dA, want_dB), start):
         assert np.linalg.norm(f64(got) - (want + s)) <= 2e-6 * np.linalg.norm(want)
+
+
+# ---- the ends of the range of numbers ---------------------------------------------------------------------------------------------------
+
+LARGEST = torch.finfo(torch.float32).max                     # bf16's largest number is 0.4 % smaller
+
+
+@pytest.mark.parametrize("n,inner,outer", [(8, 64, 64), (200, 64, 64), (600, 100, 104), (17000, 72, 520), (66000, 64, 40)])
+def test_fp32_factors_up_to_the_largest_number(n, inner, outer):
+    """One of them in each factor of every product; the results are finite."""
+    gen = torch.Generator().manual_seed(n)
+    small = lambda *shape: torch.randn(*shape, generator=gen).clamp(-3, 3) * 1e-3
+    x, dy, W = small(n, inner), small(n, outer), small(3, outer, inner)
+    x[1, inner // 2], dy[n // 2, 2] = LARGEST, -LARGEST
+    W[1, 1, 0], W[0, 3, 5] = -LARGEST, LARGEST * 0.998
+    x, dy, W, off = x.cuda(), dy.cuda(), W.cuda(), [0, n // 3, n // 2, n]
+    layer = nb.make_layer("f32", 3, inner, outer)
+    y, dx, dW = empty(n, outer, outer, "f32"), empty(n, inner, inner, "f32"), torch.zeros(3, outer, inner, device="cuda")
+    nb.grouped_fwd(layer, x, W, on_device(off), y)
+    q, e = torch.zeros(n, (inner + 31) // 32 * 32, dtype=torch.int8, device="cuda"), torch.zeros(n, (inner + 31) // 32, dtype=torch.uint8, device="cuda")
+    nb.pack8(x, q, e)
+    sizes = [np.abs(f64(t)) for t in (x, W, dy)]
+    check(y, lo.grouped_forward(f64(x), f64(W), off), lo.grouped_forward(sizes[0], sizes[1], off), "f32", inner, "y")
+    for given, kept in ((x, f64(x)), ((q, e), lo.unpack8(q.cpu().numpy(), e.cpu().numpy(), inner))):
+        nb.grouped_bwd(layer, given, W, on_device(off), dy, dx, dW, torch.zeros(max(nb.grouped_workspace_bytes(layer, n) // 4, 4), device="cuda"))
+        want_dx, want_dW = lo.grouped_backward(kept, f64(W), off, f64(dy))
+        size_dx, size_dW = lo.grouped_backward(np.abs(kept), sizes[1], off, sizes[2])
+        check(dx, want_dx, size_dx, "f32", outer, "dx")
+        check(dW, want_dW, size_dW, "f32", n, "dW")
+
+
+@pytest.mark.parametrize("n,inner,outer,rank", [(8, 64, 64, 8), (200, 64, 64, 8), (600, 100, 104, 20), (17000, 72, 520, 8), (66000, 64, 40, 8)])
+def test_adapters_up_to_the_largest_number(n, inner, outer, rank):
+    gen = torch.Generator().manual_seed(n + rank)
+    small = lambda *shape: torch.randn(*shape, generator=gen).clamp(-3, 3) * 1e-3
+    x, dy, W, A, B = small(n, inner), small(n, outer), small(outer, inner), small(3, rank, inner), small(3, outer, rank)
+    x[1, inner // 2], dy[0, 2], W[1, 0], A[1, 2, 3], B[2, 4, 1] = LARGEST, -LARGEST, LARGEST, -LARGEST, LARGEST
+    x, dy, W, A, B = (t.cuda() for t in (x, dy, W, A, B))
+    off, slots, scales = [0, n // 3, n // 2, n], [0, 1, 2], torch.ones(3, device="cuda")
+    layer = nb.make_layer("f32", 3, inner, outer, rank=rank, adapters=3)
+    y, u, dx = empty(n, outer, outer, "f32"), torch.zeros(n, rank, device="cuda"), empty(n, inner, inner, "f32")
+    dA, dB = torch.zeros_like(A), torch.zeros_like(B)
+    nb.adapter_fwd(layer, x, W, A, B, scales, on_device(slots), on_device(off), u, y)
+    nb.adapter_bwd(layer, x, W, A, B, scales, on_device(slots), on_device(off), u, dy, dx, dA, dB,
+                   torch.zeros(nb.adapter_workspace_bytes(layer, n) // 4, device="cuda"))
+    args, sizes = [f64(t) for t in (x, W, A, B)], [np.abs(f64(t)) for t in (x, W, A, B)]
+    rest = ([1.0] * 3, slots, off)
+    want, size = lo.adapter_forward(*args, *rest), lo.adapter_forward(*sizes, *rest)
+    check(u, want[1], size[1], "f32", inner, "u")
+    check(y, want[0], size[0], "f32", 2 * inner + rank, "y")
+    want, size = lo.adapter_backward(*args, *rest, f64(u), f64(dy)), lo.adapter_backward(*sizes, *rest, np.abs(f64(u)), np.abs(f64(dy)))
+    check(dx, want[0], size[0], "f32", 2 * outer + rank, "dx")
+    check(dA, want[1], size[1], "f32", n + outer, "dA")
+    check(dB, want[2], size[2], "f32", n, "dB")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,inner,outer", [(16, 64, 64), (300, 64, 64), (17000, 72, 520), (8400, 64, 1024), (8400, 1024, 64)])
+def test_u_and_v_up_to_the_largest_number_beside_16_bit_matrices(n, inner, outer, dtype):
+    """u = v = a scale above bf16's largest number, times 2^-10 in y, dx, dA and dB.  Everything is one product: off by its rounding alone
+    (fp16: y and dx are beyond its numbers)."""
+    rank, scales = 8, torch.tensor([LARGEST * 0.999], device="cuda")
+    want = float(scales.double()) * 2.0 ** -10
+    layer = nb.make_layer(dtype, 1, inner, outer, rank=rank, adapters=1)
+    new = lambda *shape: torch.zeros(*shape, dtype=TYPES[dtype], device="cuda")
+    W, off, workspace = new(outer, inner), on_device([0, n]), torch.zeros(nb.adapter_workspace_bytes(layer, n) // 4, device="cuda")
+    near = lambda got, room: bool(torch.all(torch.isinf(got) if got.dtype == torch.float16 else (got.double() / want - 1.0).abs() <= room))
+    # u = s in every row; row 5's dy takes it into dB
+    x, dy, A, B = new(n, inner), new(n, outer), new(1, rank, inner), new(1, outer, rank)
+    x[:, 0], A[0, 0, 0], B[0, :, 0], dy[5, 1] = 1.0, 1.0, 2.0 ** -10, 2.0 ** -10
+    u, y = torch.zeros(n, rank, device="cuda"), empty(n, outer, outer, dtype)
+    nb.adapter_fwd(layer, x, W, A, B, scales, None, off, u, y)
+    assert torch.all(u[:, 0] == scales) and not u[:, 1:].any() and near(y, 2.0 ** -8)
+    dA, dB = torch.zeros(A.shape, device="cuda"), torch.zeros(B.shape, device="cuda")
+    nb.adapter_bwd(layer, x, W, A, new(1, outer, rank), scales, None, off, u, dy, None, dA, dB, workspace)
+    assert near(dB[0, 1, 0], 2.0 ** -23) and dB.count_nonzero() == 1 and not dA.any()
+    # v = s in every row; row 5's x takes it into dA
+    x, dy, A, B = new(n, inner), new(n, outer), new(1, rank, inner), new(1, outer, rank)
+    dy[:, 0], B[0, 0, 0], A[0, 0, :], x[5, 1] = 1.0, 1.0, 2.0 ** -10, 2.0 ** -10
+    dx = empty(n, inner, inner, dtype)
+    nb.adapter_bwd(layer, x, W, A, B, scales, None, off, torch.zeros_like(u), dy, dx, dA, dB, workspace)
+    assert near(dx, 2.0 ** -8) and near(dA[0, 0, 1], 2.0 ** -23) and dA.count_nonzero() == 1 and not dB.any()
