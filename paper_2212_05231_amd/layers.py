@@ -2,7 +2,8 @@
 matrices for each frame, view or block of space instead of one for the whole batch), trained with first-order gradients.
 
 Every layer has one matrix per group of consecutive rows, or one matrix for all rows and a low-rank adapter per group.  For the
-backward pass it keeps its input in 8 bits and the ReLU masks in single bits (9.25 bits a feature instead of 32), or as it is.
+backward pass it keeps its input in 8 bits and the ReLU masks in single bits (9.25 bits a feature instead of 32), or as it is;
+activations that are kept in 8 bits, and gradients, pass from layer to layer through two buffers.
 This module orders calls of the library and owns the buffers; all arithmetic is in the library.
 """
 from __future__ import annotations
@@ -42,8 +43,12 @@ class RowNetwork:
             self.layer.append(nb.make_layer(dtype, groups, dims[l], dims[l + 1], rank=rank, adapters=bank, relu=not last))
             self.dense.append(nb.make_layer(dtype, 1, dims[l], dims[l + 1]))
         rows = lambda width: torch.zeros(n, width, dtype=self.tdt, device=device)
-        self.rows = [None] + [rows(d) for d in dims[1:]]                   # activations: the input of layer l is rows[l]
-        self.grad = [rows(d) for d in dims[:-1]] + [None]
+        # what one layer hands to the next and nobody needs afterwards: two buffers in turn
+        turns = [torch.zeros(n * max(dims[1:-1], default=0), dtype=self.tdt, device=device) for _ in range(4 if keep8 else 2)]
+        in_turn = lambda l, at: turns[at + l % 2][:n * dims[l]].view(n, dims[l])
+        # activations (the input of layer l is rows[l]) and the gradients with respect to them
+        self.rows = [None] + [in_turn(l, 2) if keep8 else rows(dims[l]) for l in range(1, len(dims) - 1)] + [rows(dims[-1])]
+        self.grad = [rows(dims[0])] + [in_turn(l, 0) for l in range(1, len(dims) - 1)] + [None]
         packed = lambda d: (torch.zeros(n, (d + 31) // 32 * 32, dtype=torch.int8, device=device),
                             torch.zeros(n, (d + 31) // 32, dtype=torch.uint8, device=device))
         self.kept = [packed(d) for d in dims[:-1]] if keep8 else None

@@ -8,6 +8,7 @@ torch = pytest.importorskip("torch")
 
 from oracle import layers_oracle as lo
 from paper_2212_05231_amd import binding as nb
+from paper_2212_05231_amd import layers as rows_layers
 from test_gpu_layers import MARK, TYPES, check, empty, f64, nan_to, on_device, rows, split_rows
 
 pytestmark = pytest.mark.gpu
@@ -204,3 +205,60 @@ def test_u_and_v_up_to_the_largest_number_beside_16_bit_matrices(n, inner, outer
     dx = empty(n, inner, inner, dtype)
     nb.adapter_bwd(layer, x, W, A, B, scales, None, off, torch.zeros_like(u), dy, dx, dA, dB, workspace)
     assert near(dx, 2.0 ** -8) and near(dA[0, 0, 1], 2.0 ** -23) and dA.count_nonzero() == 1 and not dB.any()
+
+
+# ---- networks --------------------------------------------------------------------------------------------------------------------------
+
+def deep_network(keep8, adapters, seed, **kw):
+    rng = np.random.default_rng(seed)
+    dims, groups, n = [40, 64, 128, 128, 64, 24, 3], 4, 333
+    pairs = list(zip(dims[1:], dims[:-1]))
+    draw = lambda *shape: rng.normal(size=shape) * (2.0 / shape[-1]) ** 0.5
+    mats = [draw(o, i) if adapters else draw(groups, o, i) for o, i in pairs]
+    bank = [(draw(2, 4, i), draw(2, o, 4), np.array([1.0, 0.5])) for o, i in pairs] if adapters else None
+    if keep8 is not None:
+        kw["keep8"] = keep8
+    net = rows_layers.RowNetwork(dims, n, groups, mats, "f32", bank, [0, 1, -1, 0] if adapters else None, **kw)
+    x, dy = torch.as_tensor(rng.normal(size=(n, dims[0]))).float().cuda(), torch.as_tensor(rng.normal(size=(n, 3)) * 0.01).float().cuda()
+    return net, dims, x, dy, on_device([0, 100, 101, 250, 333])
+
+
+@pytest.mark.parametrize("adapters", [False, True])
+@pytest.mark.parametrize("keep8", [False, True])
+def test_deep_networks_whose_layers_share_buffers(keep8, adapters):
+    """Six layers: the bits of the same calls with a buffer of its own for everything, for a second batch and its gradients too."""
+    net, dims, x, dy, off = deep_network(keep8, adapters, 21)
+    n, count = net.n, len(dims) - 1
+    for batch in range(2):
+        y = net.forward(x, off)
+        dx = net.backward(dy, want_dx=True)
+        h, inputs, masks, us = x, [], [], []
+        for l in range(count):
+            blocks = (dims[l] + 31) // 32
+            q, e, m = (torch.zeros(n, w, dtype=t, device="cuda") for w, t in ((32 * blocks, torch.int8), (blocks, torch.uint8), (blocks, torch.int32)))
+            nb.pack8(h, q, e, m)
+            inputs.append((q, e) if keep8 else h)
+            masks.append(m if l > 0 else None)
+            out, u = torch.zeros(n, dims[l + 1], device="cuda"), torch.zeros(n, 4, device="cuda")
+            if adapters:
+                nb.adapter_fwd(net.layer[l], h, net.W[l], *net.adapters[l], net.slots, off, u, out)
+            else:
+                nb.grouped_fwd(net.layer[l], h, net.W[l], off, out)
+            us.append(u)
+            h = out
+        assert torch.equal(y, h)
+        d = dy
+        for l in reversed(range(count)):
+            down, dW, ws = torch.zeros(n, dims[l], device="cuda"), torch.zeros_like(net.dW[l]), torch.zeros_like(net.workspace)
+            if adapters:
+                A, B, scales = net.adapters[l]
+                dA, dB = torch.zeros_like(net.dA[l]), torch.zeros_like(net.dB[l])
+                nb.adapter_bwd(net.layer[l], inputs[l], net.W[l], A, B, scales, net.slots, off, us[l], d, down, dA, dB, ws, masks=masks[l])
+                nb.grouped_bwd(net.dense[l], inputs[l], None, None, d, None, dW.unsqueeze(0), ws)
+                assert torch.equal(dA, net.dA[l]) and torch.equal(dB, net.dB[l]), l
+            else:
+                nb.grouped_bwd(net.layer[l], inputs[l], net.W[l], off, d, down, dW, ws, masks=masks[l])
+            assert torch.equal(dW, net.dW[l]) and dW.any(), l
+            d = down
+        assert torch.equal(dx, d)
+        x, dy = x.flip(0).contiguous(), dy * 2

@@ -226,3 +226,50 @@ def test_a_refused_backward_call_has_launched_nothing():
     """More workgroups for dW than there are numbers: refused before dx is written, not after (without a GPU that launch would fail first)."""
     l = layer(dtype="bf16", groups=1 << 16, out_dim=65536, in_dim=65536)
     assert grouped_bwd(l, n=1 << 16) == -2 and b"workgroups" in nb.lib().neus2_last_error()
+
+
+# ---- the network that owns its buffers -----------------------------------------------------------------------------------------
+
+def host_network(dims, n, groups, adapters=False, **kw):
+    torch = pytest.importorskip("torch")
+    from paper_2212_05231_amd import layers as rows_layers
+    pairs = list(zip(dims[1:], dims[:-1]))
+    mats = [torch.ones(o, i) if adapters else torch.ones(groups, o, i) for o, i in pairs]
+    bank = [(torch.ones(3, 4, i), torch.ones(3, o, 4), torch.ones(3)) for o, i in pairs] if adapters else None
+    return rows_layers.RowNetwork(dims, n, groups, mats, "f32", bank, device="cpu", **kw), mats, bank
+
+
+def held_bytes(thing, seen):
+    """Bytes of all tensors that an object, list or tuple holds, every allocation once."""
+    torch = pytest.importorskip("torch")
+    if isinstance(thing, torch.Tensor):
+        storage = thing.untyped_storage()
+        new = storage.data_ptr() not in seen
+        seen.add(storage.data_ptr())
+        return storage.nbytes() if new else 0
+    if isinstance(thing, dict):
+        thing = list(thing.values())
+    return sum(held_bytes(t, seen) for t in thing) if isinstance(thing, (list, tuple)) else 0
+
+
+@pytest.mark.parametrize("adapters", [False, True])
+@pytest.mark.parametrize("dims", [[64] * 9, [40, 64, 128, 128, 64, 24, 3]])
+def test_a_network_that_keeps_8_bits_holds_less(dims, adapters):
+    """A row costs 9.25 bits a feature kept, beside the input's gradient, the output and two buffers in turn for the activations and for
+    their gradients; without 8 bits 32 a feature and a mask."""
+    n = 512
+    eight, _, _ = host_network(dims, n, 5, adapters, keep8=True)
+    full, _, _ = host_network(dims, n, 5, adapters, keep8=False)
+    blocks = [(d + 31) // 32 for d in dims]
+    masks, ends, turn = 4 * sum(blocks[1:-1]), 4 * (dims[0] + dims[-1]), 4 * max(dims[1:-1])
+    rows_of = lambda net: held_bytes([net.rows, net.grad, net.kept or [], net.masks], set())
+    assert rows_of(eight) == n * (33 * sum(blocks[:-1]) + masks + ends + 4 * turn)
+    assert rows_of(full) == n * (4 * sum(dims[1:-1]) + masks + ends + 2 * turn)
+    assert held_bytes(eight.__dict__, set()) < held_bytes(full.__dict__, set())
+    # nothing that is still needed lies in the place of something else
+    for net in (eight, full):
+        for buffers in (net.rows[1:], net.grad[:-1]):
+            for a, b in zip(buffers, buffers[1:]):
+                assert a.data_ptr() != b.data_ptr() and a.shape[0] == b.shape[0] == n
+        assert not {t.data_ptr() for t in net.rows[1:]} & {t.data_ptr() for t in net.grad[:-1]}
+        assert all(t.shape[1] == d for t, d in zip(net.rows[1:], dims[1:])) and all(t.shape[1] == d for t, d in zip(net.grad[:-1], dims[:-1]))
