@@ -2,8 +2,8 @@
 matrices for each frame, view or block of space instead of one for the whole batch), trained with first-order gradients.
 
 Every layer has one matrix per group of consecutive rows, or one matrix for all rows and a low-rank adapter per group.  For the
-backward pass it keeps its input in 8 bits and the ReLU masks in single bits (9.25 bits a feature instead of 32), or as it is;
-activations that are kept in 8 bits, and gradients, pass from layer to layer through two buffers.
+backward pass it keeps its input as it is, or in 8 bits where the caller wants that, and the ReLU masks in single bits (9.25 bits a
+feature instead of 33); activations that are kept in 8 bits, and gradients, pass from layer to layer through two buffers.
 This module orders calls of the library and owns the buffers; all arithmetic is in the library.
 """
 from __future__ import annotations
@@ -15,10 +15,12 @@ from . import binding as nb
 
 class RowNetwork:
     def __init__(self, dims: Sequence[int], n: int, groups: int, matrices, dtype: str = "f32", adapters=None, slots=None,
-                 keep8: bool = True, train_matrices: bool = True, device="cuda"):
+                 keep8: bool = False, train_matrices: bool = True, device="cuda"):
         """`n` rows in every batch, all of them in some group.  `dims`: widths, input first.  `matrices[l]`: [groups, dims[l+1], dims[l]], or with adapters [dims[l+1], dims[l]].
         `adapters[l]`: (A [bank, rank, dims[l]], B [bank, dims[l+1], rank], scales [bank]); `slots` [groups] the adapter of
-        each group (None: its own number).  `train_matrices`: False leaves shared matrices as they are (adapters only)."""
+        each group (None: its own number).  `keep8`: layer inputs are kept in 8 bits, and matrix gradients are those of the
+        rounded inputs (each off by at most 1/127 of the largest of its 32).  `train_matrices`: False leaves shared matrices as
+        they are (adapters only)."""
         import torch
         self.torch, self.dims, self.n, self.groups, self.dtype = torch, list(dims), n, groups, dtype
         self.layers_count = len(dims) - 1

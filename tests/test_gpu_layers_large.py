@@ -262,3 +262,18 @@ def test_deep_networks_whose_layers_share_buffers(keep8, adapters):
             d = down
         assert torch.equal(dx, d)
         x, dy = x.flip(0).contiguous(), dy * 2
+
+
+def test_networks_round_nothing_to_8_bits_unless_told():
+    """Gradients of a network made without further arguments are those of its activations as they are (in 8 bits: off by 1e-3 and more)."""
+    net, dims, x, dy, off = deep_network(None, False, 22)
+    net.forward(x, off)
+    net.backward(dy)
+    ends, h, kept = off.tolist(), f64(x), []
+    for l in range(len(dims) - 1):
+        kept.append(h)
+        h = lo.grouped_forward(h, f64(net.W[l]), ends, l + 2 < len(dims))
+    d = f64(dy)
+    for l in reversed(range(len(dims) - 1)):
+        d, dW = lo.grouped_backward(kept[l], f64(net.W[l]), ends, d, kept[l] > 0 if l > 0 else None)
+        assert np.linalg.norm(f64(net.dW[l]) - dW) <= 5e-6 * np.linalg.norm(dW), l
