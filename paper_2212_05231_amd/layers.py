@@ -28,14 +28,16 @@ class RowNetwork:
             raise ValueError(f"{self.layers_count} layers need as many matrices and adapters")
         self.keep8, self.train_matrices, self.device = keep8, train_matrices or adapters is None, device
         self.tdt = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
-        move = lambda t: torch.as_tensor(t).to(device=device, dtype=self.tdt).contiguous()
+        # copies: training changes the network's matrices, not the caller's
+        own = lambda t, dtype: torch.as_tensor(t).detach().to(device=device, dtype=dtype, copy=True).contiguous()
+        move = lambda t: own(t, self.tdt)
         f32 = dict(dtype=torch.float32, device=device)
         self.W = [move(m) for m in matrices]
         self.dW = [torch.zeros(w.shape, **f32) if self.train_matrices else None for w in self.W]
-        self.slots = None if slots is None else torch.as_tensor(slots, dtype=torch.int32).to(device)
+        self.slots = None if slots is None else own(slots, torch.int32)
         self.adapters = None
         if adapters is not None:
-            self.adapters = [(move(A), move(B), torch.as_tensor(s, dtype=torch.float32).to(device)) for A, B, s in adapters]
+            self.adapters = [(move(A), move(B), own(s, torch.float32)) for A, B, s in adapters]
             self.dA = [torch.zeros(A.shape, **f32) for A, _, _ in self.adapters]
             self.dB = [torch.zeros(B.shape, **f32) for _, B, _ in self.adapters]
         self.layer, self.dense = [], []

@@ -273,3 +273,19 @@ def test_a_network_that_keeps_8_bits_holds_less(dims, adapters):
                 assert a.data_ptr() != b.data_ptr() and a.shape[0] == b.shape[0] == n
         assert not {t.data_ptr() for t in net.rows[1:]} & {t.data_ptr() for t in net.grad[:-1]}
         assert all(t.shape[1] == d for t, d in zip(net.rows[1:], dims[1:])) and all(t.shape[1] == d for t, d in zip(net.grad[:-1], dims[:-1]))
+
+
+def test_a_network_owns_its_matrices():
+    """Training steps change the network's matrices, not what it was made from; two networks made from the same tensors share nothing."""
+    torch = pytest.importorskip("torch")
+    one, mats, bank = host_network([20, 30, 10], 8, 3, True, slots=torch.zeros(3, dtype=torch.int32))
+    from paper_2212_05231_amd import layers as rows_layers
+    slots = torch.tensor([0, 1, 2], dtype=torch.int32)
+    two = rows_layers.RowNetwork([20, 30, 10], 8, 3, [mats[0], mats[1]], "f32", bank, slots, device="cpu")
+    given = {t.data_ptr() for t in mats + [t for a in bank for t in a] + [slots]}
+    held = [[t.data_ptr() for t in net.W + [t for a in net.adapters for t in a] + [net.slots]] for net in (one, two)]
+    assert not given & set(held[0] + held[1]) and not set(held[0]) & set(held[1])
+    for t, mat in zip(one.W, mats):
+        assert torch.equal(t, mat)
+        t.fill_(7.0)
+        assert torch.all(mat == 1.0)
