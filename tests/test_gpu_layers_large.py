@@ -277,3 +277,186 @@ def test_networks_round_nothing_to_8_bits_unless_told():
     for l in reversed(range(len(dims) - 1)):
         d, dW = lo.grouped_backward(kept[l], f64(net.W[l]), ends, d, kept[l] > 0 if l > 0 else None)
         assert np.linalg.norm(f64(net.dW[l]) - dW) <= 5e-6 * np.linalg.norm(dW), l
+
+
+# ---- the kernels of large calls ------------------------------------------------------------------------------------------------------------
+# On 256 compute units: workgroups that take a second tile (narrow ones from 98304 rows on, wide ones from 257 tiles of 256 x 256 on) and
+# the quarters of a last round; tiles of 128 x 64 and 128 x 128 (512 of them); outputs of more and of less than 32 MB.
+
+GROUPED = [  # dtypes, n, groups, inner, outer, pad, before, behind, none
+    ("f32", 140003, 20, 64, 64, 0, 0, 0, 3), ("f32 f16", 110000, 300, 40, 24, 8, 77, 130, 60), ("f16 bf16", 270000, 20, 64, 64, 0, 0, 0, 0),
+    ("f32 bf16", 66000, 3, 100, 48, 0, 0, 5, 0), ("f32 f16", 66000, 3, 48, 100, 4, 0, 0, 0),
+    ("f32", 17000, 4, 72, 520, 0, 9, 0, 0), ("f32", 17000, 4, 520, 72, 0, 0, 0, 1), ("f16", 33000, 2, 72, 520, 8, 0, 0, 0),
+    ("f16 bf16", 20000, 1, 64, 1024, 0, 0, 0, 0), ("bf16", 20000, 1, 1024, 64, 0, 0, 0, 0), ("f16 bf16", 20000, 5, 192, 1000, 0, 100, 33, 1),
+    ("f16 bf16", 20000, 5, 1000, 192, 8, 100, 33, 1), ("bf16", 20000, 6, 128, 1032, 8, 0, 0, 0), ("f16", 20000, 6, 1032, 128, 0, 0, 0, 0),
+    ("f16 bf16", 34000, 3, 64, 264, 0, 0, 300, 0), ("f16", 34000, 3, 264, 64, 0, 0, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype,shape", [(t, s[1:]) for s in GROUPED for t in s[0].split()], ids=lambda v: v if isinstance(v, str) else "x".join(map(str, v[:4])))
+def test_grouped_rows_of_large_calls(shape, dtype):
+    n, groups, inner, outer, pad, before, behind, none = shape
+    gen = torch.Generator().manual_seed(n + inner)
+    off = split_rows(n, groups, gen, before, behind, none) if groups > 1 else [0, n]
+    x, dy = rows(n, inner, inner + pad, dtype, gen), rows(n, outer, outer + pad, dtype, gen, 0.01)
+    for t in (x, dy):
+        t[:before], t[n - behind:] = float("nan"), float("inf")
+    W = (torch.randn(groups, outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    layer = nb.make_layer(dtype, groups, inner, outer, relu=True, x_stride=inner + pad, y_stride=outer + pad)
+    kept = torch.rand(n, inner, generator=gen) < 0.5
+    masks = torch.as_tensor(lo.mask_words(kept.numpy())).cuda()
+    y, dx = empty(n, outer, outer + pad, dtype), empty(n, inner, inner + pad, dtype)
+    nb.grouped_fwd(layer, x, W, on_device(off), y)
+    nb.grouped_bwd(layer, None, W, on_device(off), dy, dx, None, masks=masks)
+    for t, width in ((y, outer), (dx, inner)):
+        assert pad == 0 or torch.all(t.as_strided((n, pad), (width + pad, 1), width) == MARK)
+    only = lambda a: np.where(np.isfinite(a), a, 0.0)                  # rows of nobody
+    check(y, lo.grouped_forward(f64(x), f64(W), off, True), lo.grouped_forward(np.abs(only(f64(x))), np.abs(f64(W)), off), dtype, inner, "y")
+    # dx of rows is the forward product of dy with the transposed matrices
+    Wt = f64(W).transpose(0, 2, 1)
+    want, size = lo.grouped_forward(f64(dy), Wt, off), lo.grouped_forward(np.abs(only(f64(dy))), np.abs(Wt), off)
+    check(dx, np.where(kept.numpy() | np.isnan(want), want, 0.0), size, dtype, outer, "dx")
+
+
+@pytest.mark.parametrize("dtype,n,groups,inner,outer,accumulate", [("f32", 140003, 20, 64, 64, 0), ("f16", 270000, 20, 64, 64, 1), ("bf16", 270000, 7, 56, 40, 0)])
+def test_narrow_gradients_of_large_calls(dtype, n, groups, inner, outer, accumulate):
+    """Both gradients in one pass, dx of more than 32 MB (the last case less), inputs in 8 bits and masks."""
+    gen = torch.Generator().manual_seed(n)
+    off = split_rows(n, groups, gen, 50, 70, 2)
+    x, dy = rows(n, inner, inner, dtype, gen, relu=True), rows(n, outer, outer, dtype, gen, 0.01)
+    W = (torch.randn(groups, outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    blocks = (inner + 31) // 32
+    q, e, masks = (torch.zeros(n, w, dtype=t, device="cuda") for w, t in ((32 * blocks, torch.int8), (blocks, torch.uint8), (blocks, torch.int32)))
+    nb.pack8(x, q, e, masks)
+    x64 = lo.unpack8(q.cpu().numpy(), e.cpu().numpy(), inner)
+    layer = nb.make_layer(dtype, groups, inner, outer, accumulate=bool(accumulate))
+    workspace = torch.full((nb.grouped_workspace_bytes(layer, n) // 4,), float("nan"), device="cuda")
+    dx, dW = empty(n, inner, inner, dtype), torch.randn(groups, outer, inner, generator=gen).cuda()
+    start = f64(dW) if accumulate else 0.0
+    nb.grouped_bwd(layer, (q, e), W, on_device(off), dy, dx, dW, workspace, masks=masks)
+    want_dx, want_dW = lo.grouped_backward(x64, f64(W), off, f64(dy), f64(x) > 0)
+    size_dx, size_dW = lo.grouped_backward(np.abs(x64), np.abs(f64(W)), off, np.abs(f64(dy)))
+    check(dx, want_dx, size_dx, dtype, outer, "dx")
+    check(dW, want_dW + start, size_dW + np.abs(start), "f32", max(b - a for a, b in zip(off, off[1:])), "dW")
+
+
+@pytest.mark.parametrize("packed,accumulate", [(False, 1), (True, 0)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,groups,inner,outer", [(8300, 64, 264, 304), (66000, 1, 304, 264), (70000, 3, 296, 520)])
+def test_wide_sums_of_partly_filled_tiles(n, groups, inner, outer, dtype, packed, accumulate):
+    """dW in tiles of 256 x 256 that end inside the matrix, less than 32 MB of them; groups of one chunk and of many."""
+    gen = torch.Generator().manual_seed(n)
+    off = split_rows(n, groups, gen, 3, 5, 1) if groups > 1 else [0, n]
+    x, dy = rows(n, inner, inner + 8, dtype, gen), rows(n, outer, outer, dtype, gen, 0.01)
+    layer = nb.make_layer(dtype, groups, inner, outer, accumulate=bool(accumulate), x_stride=inner + 8)
+    blocks = (inner + 31) // 32
+    q, e = torch.zeros(n, 32 * blocks, dtype=torch.int8, device="cuda"), torch.zeros(n, blocks, dtype=torch.uint8, device="cuda")
+    nb.pack8(x, q, e)
+    x64 = lo.unpack8(q.cpu().numpy(), e.cpu().numpy(), inner) if packed else f64(x)
+    dW = torch.randn(groups, outer, inner, generator=gen).cuda()
+    start = f64(dW) if accumulate else 0.0
+    workspace = torch.full((max(nb.grouped_workspace_bytes(layer, n) // 4, 4),), float("nan"), device="cuda")
+    nb.grouped_bwd(layer, (q, e) if packed else x, None, on_device(off), dy, None, dW, workspace)
+    want, size, dy64 = np.zeros(dW.shape), np.zeros(dW.shape), f64(dy)
+    for g in range(groups):
+        part = slice(off[g], off[g + 1])
+        want[g], size[g] = dy64[part].T @ x64[part], np.abs(dy64[part]).T @ np.abs(x64[part])
+    check(dW, want + start, size + np.abs(start), "f32", max(b - a for a, b in zip(off, off[1:])), "dW")
+
+
+ADAPTED = [  # dtypes, n, groups, slots, inner, outer, rank, pad, before, behind
+    ("f32 f16 bf16", 66000, 49, 30, 64, 64, 8, 0, 0, 9), ("f32 f16", 17000, 9000, 5, 72, 520, 20, 0, 4, 0), ("f32 bf16", 17000, 40, 12, 520, 72, 16, 0, 0, 0),
+    ("f16 bf16", 8400, 150, 40, 64, 1024, 16, 8, 0, 0), ("f16 bf16", 8400, 4200, 7, 1024, 64, 20, 0, 10, 20), ("bf16", 16500, 3, 3, 128, 1024, 33, 0, 0, 0),
+    ("f16", 16500, 24, 20, 1024, 128, 64, 0, 5, 5), ("f16 bf16", 8400, 24, 6, 192, 1000, 64, 0, 0, 100), ("bf16", 8400, 24, 6, 1000, 192, 12, 0, 0, 0)]
+
+
+def large_adapters(shape, dtype, seed):
+    n, groups, slots, inner, outer, rank, pad, before, behind = shape
+    gen = torch.Generator().manual_seed(seed)
+    off, named = split_rows(n, groups, gen, before, behind), torch.randint(-1, slots + 1, (groups,), generator=gen)
+    x, dy = rows(n, inner, inner + pad, dtype, gen), rows(n, outer, outer + pad, dtype, gen, 0.01)
+    W = (torch.randn(outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    A = (torch.randn(slots, rank, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    B = (torch.randn(slots, outer, rank, generator=gen) * rank ** -0.5).to(TYPES[dtype]).cuda()
+    return off, named.tolist(), x, dy, W, A, B, (torch.rand(slots, generator=gen) + 0.5).cuda(), gen
+
+
+@pytest.mark.parametrize("dtype,shape", [(t, s[1:]) for s in ADAPTED for t in s[0].split()], ids=lambda v: v if isinstance(v, str) else "x".join(map(str, v[:6])))
+def test_adapters_of_large_calls(shape, dtype):
+    """Tiles of 128 x 64, 128 x 128 and 256 x 256 that hold parts of segments, whole ones and more than 64 of them; forward and every gradient."""
+    n, groups, slots, inner, outer, rank, pad, before, behind = shape
+    off, named, x, dy, W, A, B, scales, gen = large_adapters(shape, dtype, n + rank)
+    layer = nb.make_layer(dtype, groups, inner, outer, rank=rank, adapters=slots, relu=True, x_stride=inner + pad, y_stride=outer + pad)
+    y, u, dx = empty(n, outer, outer + pad, dtype), torch.full((n, rank), MARK, device="cuda"), empty(n, inner, inner + pad, dtype)
+    kept = torch.rand(n, inner, generator=gen) < 0.5
+    masks = torch.as_tensor(lo.mask_words(kept.numpy())).cuda()
+    nb.adapter_fwd(layer, x, W, A, B, scales, on_device(named), on_device(off), u, y)
+    args, sizes = [f64(t) for t in (W, A, B, scales)], [np.abs(f64(t)) for t in (W, A, B, scales)]
+    want, size = lo.adapter_forward(f64(x), *args, named, off, True), lo.adapter_forward(np.abs(f64(x)), *sizes, named, off)
+    check(u, want[1], size[1], "f32", inner, "u")
+    check(y, want[0], size[0], dtype, 2 * inner + rank, "y")
+    dA, dB = torch.zeros(A.shape, device="cuda"), torch.zeros(B.shape, device="cuda")
+    workspace = torch.full((nb.adapter_workspace_bytes(layer, n) // 4,), float("nan"), device="cuda")
+    nb.adapter_bwd(layer, x, W, A, B, scales, on_device(named), on_device(off), u, dy, dx, dA, dB, workspace, masks=masks)
+    want, size = lo.adapter_backward(f64(x), *args, named, off, f64(u), f64(dy), kept.numpy()), lo.adapter_backward(
+        np.abs(f64(x)), *sizes, named, off, np.abs(f64(u)), np.abs(f64(dy)))
+    check(dx, want[0], size[0], dtype, 2 * outer + rank, "dx")
+    check(dA, want[1], size[1], "f32", n + outer, "dA")
+    check(dB, want[2], size[2], "f32", n, "dB")
+
+
+@pytest.mark.parametrize("dtype,n,inner,outer,rank", [("f32", 66000, 64, 64, 8), ("f32", 17000, 72, 520, 20), ("f32", 17000, 520, 72, 20), ("f16", 17000, 72, 520, 20),
+                                                      ("f16", 8400, 64, 1024, 16), ("bf16", 8400, 1024, 64, 16), ("bf16", 8400, 64, 1024, 40)])
+def test_an_infinite_adapter_stays_with_its_rows_in_large_tiles(dtype, n, inner, outer, rank):
+    gen = torch.Generator().manual_seed(n + rank)
+    x, dy = rows(n, inner, inner, dtype, gen), rows(n, outer, outer, dtype, gen, 0.01)
+    W = (torch.randn(outer, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    A = (torch.randn(3, rank, inner, generator=gen) * inner ** -0.5).to(TYPES[dtype]).cuda()
+    B = (torch.randn(3, outer, rank, generator=gen) * rank ** -0.5).to(TYPES[dtype]).cuda()
+    scales, off, slots = torch.ones(3, device="cuda"), [0, n // 3 + 1, n // 3 + 90, n // 3 + 100, n], [0, 1, 2, 0]
+    layer = nb.make_layer(dtype, 4, inner, outer, rank=rank, adapters=3)
+    workspace, results = torch.zeros(nb.adapter_workspace_bytes(layer, n) // 4, device="cuda"), []
+    for poison in (False, True):
+        if poison:
+            A[1, 0, 0], B[1, 1, 0], B[1, 2, 1] = float("nan"), float("inf"), -float("inf")
+        y, u, dx = empty(n, outer, outer, dtype), torch.zeros(n, rank, device="cuda"), empty(n, inner, inner, dtype)
+        dA, dB = torch.zeros(A.shape, device="cuda"), torch.zeros(B.shape, device="cuda")
+        nb.adapter_fwd(layer, x, W, A, B, scales, on_device(slots), on_device(off), u, y)
+        nb.adapter_bwd(layer, x, W, A, B, scales, on_device(slots), on_device(off), u, dy, dx, dA, dB, workspace)
+        results.append((y, u, dx, dA, dB))
+    others = torch.ones(n, dtype=torch.bool, device="cuda")
+    others[off[1]:off[2]] = False
+    for a, b in zip(results[0][:3], results[1][:3]):
+        assert torch.equal(a[others], b[others]) and not torch.isfinite(b[~others]).all(1).any()
+    for a, b in zip(results[0][3:], results[1][3:]):
+        assert torch.equal(a[[0, 2]], b[[0, 2]]) and not torch.isfinite(b[1]).all()
+
+
+@pytest.mark.parametrize("dtype,n,groups,inner,outer,rank", [("f32", 110000, 64, 64, 40, 8), ("f16", 20000, 64, 64, 1024, 16), ("bf16", 20000, 64, 1024, 64, 16),
+                                                             ("f32", 17000, 300, 72, 520, 20), ("f32", 17000, 300, 520, 72, 20)])
+def test_wrong_offsets_stay_inside_the_arrays_of_large_calls(dtype, n, groups, inner, outer, rank):
+    """Groups that each claim all rows, none, or rows that do not exist, in the kernels of the tests above."""
+    gen = torch.Generator().manual_seed(groups)
+    x, dy = rows(n, inner, inner, dtype, gen), rows(n, outer, outer, dtype, gen)
+    W = torch.randn(groups, outer, inner, generator=gen).to(TYPES[dtype]).cuda()
+    A, B = torch.randn(5, rank, inner, generator=gen).to(TYPES[dtype]).cuda(), torch.randn(5, outer, rank, generator=gen).to(TYPES[dtype]).cuda()
+    layer, adapted = nb.make_layer(dtype, groups, inner, outer), nb.make_layer(dtype, groups, inner, outer, rank=rank, adapters=5)
+    scales, named = torch.ones(5, device="cuda"), on_device([g % 7 - 1 for g in range(groups)])
+    sizes = [nb.grouped_workspace_bytes(layer, n) // 4, nb.adapter_workspace_bytes(adapted, n) // 4]
+    wild = torch.randint(-2 ** 31, 2 ** 31 - 1, (groups + 1,), generator=gen).tolist()
+    for off in ([0 if g % 2 else n for g in range(groups + 1)], [n if g % 2 else 0 for g in range(groups + 1)], [0] + wild[1:-1] + [n], wild):
+        offsets = on_device(off)
+        y, dx = (torch.full((n + 64, w), MARK, dtype=TYPES[dtype], device="cuda") for w in (outer, inner))
+        u = torch.full((n + 64, rank), MARK, device="cuda")
+        dW, dA, dB = (torch.full((k + 1, *shape), MARK, device="cuda") for k, shape in ((groups, (outer, inner)), (5, (rank, inner)), (5, (outer, rank))))
+        spaces = [torch.full((s + 256,), MARK, device="cuda") for s in sizes]
+        nb.grouped_fwd(layer, x, W, offsets, y[32:n + 32])
+        nb.grouped_bwd(layer, x, W, offsets, dy, dx[32:n + 32], dW[:groups], spaces[0][:sizes[0]] if sizes[0] else None)
+        nb.adapter_fwd(adapted, x, W[0], A, B, scales, named, offsets, u[32:n + 32], y[32:n + 32])
+        nb.adapter_bwd(adapted, x, W[0], A, B, scales, named, offsets, u[32:n + 32], dy, dx[32:n + 32], dA[:5], dB[:5], spaces[1][:sizes[1]])
+        torch.cuda.synchronize()
+        for t in (y, dx, u):
+            assert torch.all(t[:32] == MARK) and torch.all(t[n + 32:] == MARK)
+        for t in (dW, dA, dB):
+            assert torch.all(t[-1] == MARK)
+        for t, s in zip(spaces, sizes):
+            assert torch.all(t[s:] == MARK)
