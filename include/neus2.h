@@ -455,6 +455,7 @@ int neus2_march_rays(int log2_res, const uint32_t* bitfield, const float* origin
  *   x's, dy has y's.  Any stride works, multiples of 16 bytes are the fast ones.
  * accumulate: matrix gradients are ADDED into (1) or overwritten (0: groups without rows get zeros).
  * Outputs must not overlap inputs.
+ * Thousands of groups are slow: every workgroup looks through the offsets for its rows.
  * n = 0: the arrays of rows may be NULL; matrix gradients are zeroed or left as they are.
  * Results do not depend on the order in which workgroups run. */
 typedef struct neus2_layer {

@@ -7,7 +7,7 @@ namespace {
 
 // ---- the product engine ----------------------------------------------------------------------------------------------------
 // For what is neither wide nor narrow, and for fp32: bound by the waits of a round (fetch, LDS, products) where there are few tiles, by the
-// bf16 products of the fp32 terms where there are many (2048 to 2048, 2^13 rows, fp32: 362 us, 190 TFLOP/s; the library's fp32 product
+// bf16 products of the fp32 terms where there are many (2048 to 2048, 2^13 rows, fp32: 363 us, 189 TFLOP/s; the library's fp32 product
 // reaches 153 on a large matrix).
 // One workgroup owns ROWS data rows of one group and COLS outputs; both factors of DEPTH steps of the contraction lie in LDS,
 // fetched into registers while the products of the steps before run.  The matrix's tile is the instruction's first operand, so a
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(64 * WR * WC) void rows_kernel(RowsArgs a) {
 // Contractions of up to 64 steps and up to 64 outputs, the framework's own widths, with many rows: bound by reading and writing the
 // rows once.  A workgroup keeps the group's matrix in LDS, split once, and takes a run of consecutive tiles of 128 rows; a wave has 32
 // of them, whose values go from memory to registers as the instruction wants them (lane = row), the next tile's under way while this
-// one's products run.  2^18 rows, 64 to 64, fp32 in 20 groups: 26 us, 5.1 TB/s; through the tiles below 30.
+// one's products run.  2^18 rows, 64 to 64, fp32 in 20 groups: 27 us, 5.0 TB/s; with rows_kernel 30.
 constexpr int kNarrowRows = 128;
 
 template <int DT, bool BACKWARD, bool ONCE>
@@ -553,7 +553,7 @@ int launch_rows(const RowsArgs& a, hipStream_t st) {
         narrow_rows_kernel<DT, BACKWARD, ONCE><<<grid, 256, 0, st>>>(a);
     } else if (row_tiles(a.groups, 128) * ((a.cols + 127) / 128) < 2 * compute_units()) {
         // too few tiles of 128 x 128 to hide each other's waits (2048 to 2048: bf16 2^9 rows 24 us against 33, 2^11 rows 37 against 42, 2^12
-        // rows 71 against 48; fp32 2^11 rows 126 against 138, 2^12 rows 255 against 185)
+        // rows 71 against 48; fp32 2^11 rows 133 against 144, 2^12 rows 262 against 184)
         launch_tiles<DT, BACKWARD, ADAPT, ONCE, 64, 64, 2, 1>(a, st);
     } else if (a.cols > 64) {
         launch_tiles<DT, BACKWARD, ADAPT, ONCE, 128, 128, 2, 2>(a, st);
@@ -600,11 +600,13 @@ int launch_few(int dtype, FewArgs a, hipStream_t st) {
 }
 
 // Up to 16 rows a group the matrices are read once, and little else.  Up to 64 rows a group reading them once for every 16 rows, from
-// a cache, still beats the tiles as long as the workgroups are few (2048 to 2048, one group of 64 rows: bf16 10 us against 23, fp32 20
-// against 81; 8 groups of 1024 to 1024: bf16 32 rows each 13.5 against 18, 64 rows 24 against 18, fp32 64 rows 38 against 49).  Narrow layers have a kernel.
+// a cache, still beats the tiles as long as the workgroups are few (2048 to 2048, one group of 64 rows: bf16 10 us against 23, fp32 19
+// against 88; 8 groups of 1024 to 1024: bf16 32 rows each 13.5 against 18, 64 rows 24 against 18, fp32 64 rows 37 against 53).  Narrow layers have a kernel.
+// Those are equal groups.  How the rows are spread is known on the device alone, so the rule goes by their mean: 64 groups of 2048 to
+// 2048 with 1024 rows, equal ones bf16 169 against 137 with tiles, fp32 283 against 354; all rows in one group 137 against 40, 253 against 136.
 bool few_rows_fit(const neus2_layer* l, const RowGroups& g) {
     if (g.n <= 16 * (int64_t)l->groups) return true;
-    return g.n <= 64 * (int64_t)l->groups && (l->in_dim > 64 || l->out_dim > 64) && 
+    return g.n <= 64 * (int64_t)l->groups && (l->in_dim > 64 || l->out_dim > 64) &&
            row_tiles(g, 16) * ((l->out_dim + 15) / 16) <= (l->dtype == kTypeF32 ? 12 : 6) * compute_units();
 }
 
@@ -717,7 +719,7 @@ int neus2_grouped_fwd(const neus2_layer* l, const void* x, const void* W, const 
     RowsArgs a = {};
     a.groups = groups;
     a.steps = l->in_dim; a.cols = l->out_dim;
-        a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+    a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
     a.w = W; a.w_group = (int64_t)l->in_dim * l->out_dim; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
     a.y = y; a.y_stride = y_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
     a.relu = l->relu;
@@ -796,6 +798,9 @@ int neus2_adapter_fwd(const neus2_layer* l, const void* x, const void* W, const 
     hipStream_t st = (hipStream_t)stream;
     NEUS2_TRY(launch_low_rank<false>(l, x, x_stride_of(l), A, scales, slots, offsets, n, l->in_dim, u, st));
     const RowGroups whole = make_groups(offsets, l->groups, n, true);
+    // Few rows, up to 64 segments: a tile adds the adapters of its segments one after the other, few_rows_kernel a row's own (2048 to 2048,
+    // rank 16, bf16, 64 segments, with u: 64 rows 17 us against 71 with tiles; beyond the limit 65 rows 20 against 72, 128 rows 26 against
+    // 52, 256 rows 44 against 41; 16 rows in 16 segments 13 against 43; fp32 64 rows 32 against 164).
     if (n <= 64) {
         FewArgs a = {};
         a.groups = whole;
@@ -811,7 +816,7 @@ int neus2_adapter_fwd(const neus2_layer* l, const void* x, const void* W, const 
     RowsArgs a = {};
     a.groups = whole;
     a.steps = l->in_dim; a.cols = l->out_dim;
-        a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
+    a.x = x; a.x_stride = x_stride_of(l); a.x_whole = rows_whole(l->dtype, a.x_stride, a.steps);
     a.w = W; a.w_stride = l->in_dim; a.w_whole = rows_whole(l->dtype, l->in_dim, l->in_dim);
     a.y = y; a.y_stride = y_stride_of(l); a.y_vec = rows_aligned(l->dtype, a.y_stride);
     a.relu = l->relu;

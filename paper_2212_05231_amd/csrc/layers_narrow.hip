@@ -251,9 +251,9 @@ void launch(const NarrowArgs& b, bool packed, unsigned grid, hipStream_t st) {
 
 }  // namespace
 
-// A unit of 32 rows of the smallest groups must not be mostly empty, and a run must be worth a workgroup's matrix and sums: three layers
-// of 64 to 64, fp32 with inputs in 8 bits, 20 groups, 2^15 rows 70.5 us against 68.5 apart, 2^17 96 against 98, 2^18 142 against 165, 2^20
-// 365 against 552.  fp32 inputs in full take three terms more than there are registers for.
+// A unit of 32 rows of the smallest groups must not be mostly empty, and a run must be worth a workgroup's matrix and sums: layers
+// of 64 to 64, fp32 with inputs in 8 bits, 20 groups, three of them with 2^15 rows 70.5 us against 68.5 apart; one with 2^16 29 against 31,
+// 2^17 36 against 40, 2^18 46 against 55, 2^20 139 against 219.  fp32 inputs in full take three terms more than there are registers for.
 bool narrow_backward_fits(int dtype, int inner, int outer, int64_t groups, int64_t n, int64_t dy_stride, int64_t x_stride, bool packed) {
     return inner <= 64 && outer <= 64 && n >= 64 * groups && n >= (1 << 16) && (packed || dtype != kTypeF32) && rows_whole(dtype, dy_stride, outer) && rows_whole(dtype, inner, inner) &&
            (packed || rows_whole(dtype, x_stride, inner));
